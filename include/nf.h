@@ -70,7 +70,9 @@ typedef enum {
  * chosen when the library is built, real32 by default). */
 typedef enum {
   NF_F32 = 0,
-  NF_F64 = 1
+  NF_F64 = 1,
+  NF_BF16 = 2,  /* bfloat16 and fp16: data of the operators at the end of     */
+  NF_F16 = 3    /* this file only; no net has them                            */
 } nf_dtype;
 
 typedef enum {
@@ -318,6 +320,123 @@ nf_status nf_calib_copy(void* d_dst, const void* d_src, int64_t bytes, void* str
                         double* host_ms);
 nf_status nf_calib_mfma(int32_t dtype, int64_t iters, void* d_sink, void* stream,
                         double* host_ms, double* host_flops, double* host_clock_ghz);
+
+/* -- Operators for the last layers of a language model or classifier --------
+ *
+ * A loss with its gradient, an update for weight matrices and linear layers in
+ * 8-bit integers, on the caller's own arrays.  They need no net.  They run on
+ * the HIP device current at the call, which must hold the arrays; they only
+ * enqueue work on `stream`, allocate nothing and keep nothing between calls, so
+ * they may be captured in a HIP graph, and calls that share no arrays may run
+ * on several streams and threads at once.  Arrays are row-major, `ld` elements
+ * from row to row (columns <= ld; what lies between is neither read nor
+ * written), aligned to their elements.  Sums are held in fp32 or more. */
+
+/* Log probabilities, entropies and alternatives of rows of logits.
+ * With z = scale x (scale > 0: one over a temperature), m = max z and
+ * s = sum over j of exp(z_j - m):
+ *   log p_j = (z_j - m) - log s,  H = -sum over j of p_j log p_j.
+ * d_logits: [rows][classes] of dtype NF_F32, NF_BF16 or NF_F16.
+ * d_targets: [rows], or NULL.  A negative target means that the row has none:
+ *   its d_logp is 0.  One past the last class gives NaN.
+ * d_logp [rows]: log p of the target; d_entropy [rows]: H; d_stat [rows][2]: m
+ *   and log s, for nf_logprobs_grad.  Each may be NULL.
+ * n_top in 0 .. NF_TOP_MAX, at most classes: the n_top largest z of each row in
+ *   falling order, equal ones by rising class, as d_top_ids [rows][n_top] and
+ *   their log probabilities d_top_logp [rows][n_top] (either may be NULL).
+ * A class at minus infinity has probability 0 and adds nothing to H.  A row
+ * whose classes are all at minus infinity has log probabilities (and m and log
+ * s) of minus infinity and entropy 0.  A row with a NaN or plus infinity gets
+ * NaN log probabilities and entropy; NaN ranks above all numbers.
+ * rows may be 0. */
+#define NF_TOP_MAX 64
+nf_status nf_logprobs(const void* d_logits, int32_t dtype, int64_t rows, int64_t classes,
+                      int64_t ld, float scale, const int64_t* d_targets, int32_t n_top,
+                      float* d_logp, float* d_entropy, float* d_stat, int32_t* d_top_ids,
+                      float* d_top_logp, void* stream);
+
+/* The gradient with respect to the logits of
+ *   sum over rows of g log p_target + h H
+ * for weights d_g_logp [rows] and d_g_entropy [rows] (either may be NULL: 0):
+ *   dx_j = scale (g ([j = target] - p_j) - h p_j (log p_j + H)).
+ * nf_logprobs_train forms it together with log p, H and the statistics, for
+ * weights known beforehand (a mean of negative log probabilities has
+ * g = -1/rows); nf_logprobs_grad from the d_stat and, with d_g_entropy, the
+ * d_entropy of an earlier nf_logprobs on the same logits, targets and scale.
+ * d_dlogits: [rows][classes] of the logits' type, ld_d from row to row; it may
+ * be the logits' own array with the same pitch, or one apart from it.
+ * A row without a target has no g.  A target past the last class gives NaN.  A
+ * row without probabilities has gradient 0. */
+nf_status nf_logprobs_train(const void* d_logits, int32_t dtype, int64_t rows, int64_t classes,
+                            int64_t ld, float scale, const int64_t* d_targets,
+                            const float* d_g_logp, const float* d_g_entropy, float* d_logp,
+                            float* d_entropy, float* d_stat, void* d_dlogits, int64_t ld_d,
+                            void* stream);
+nf_status nf_logprobs_grad(const void* d_logits, int32_t dtype, int64_t rows, int64_t classes,
+                           int64_t ld, float scale, const int64_t* d_targets,
+                           const float* d_stat, const float* d_entropy, const float* d_g_logp,
+                           const float* d_g_entropy, void* d_dlogits, int64_t ld_d, void* stream);
+
+/* Orthogonalisation of `count` matrices of rows x cols (each at most
+ * NF_ORTH_MAX) by Newton-Schulz products: X = U / |U|_F, then NF_ORTH_STEPS times
+ *   A = X X^T,  X = a X + (b A + c A^2) X,  (a, b, c) = (3.4445, -4.7750, 2.0315)
+ * (on X^T where rows > cols), which takes U's singular values near 1 and keeps
+ * its singular vectors.  A matrix of zeros gives zeros; one with a NaN or an
+ * infinity gives NaN throughout.
+ * dtype: NF_F32 (products with fp32's precision) or NF_BF16 (products of fp16
+ * values, sums and X itself in fp32).  ld and stride: elements from row to row and from
+ * matrix to matrix; d_out may be d_x.
+ * d_work: nf_orthogonalize_work(dtype, count, rows, cols) bytes (-1 for sizes
+ * that the call would refuse) aligned to 256. */
+#define NF_ORTH_MAX 65536
+#define NF_ORTH_STEPS 5
+int64_t nf_orthogonalize_work(int32_t dtype, int64_t count, int64_t rows, int64_t cols);
+nf_status nf_orthogonalize(const void* d_x, int32_t dtype, int64_t count, int64_t rows,
+                           int64_t cols, int64_t ld, int64_t stride, void* d_out, int64_t ld_out,
+                           int64_t stride_out, void* d_work, int64_t work_bytes, void* stream);
+
+/* A step on `count` weight matrices W [rows][cols] (W_l of a net: rows = d_l,
+ * cols = d_{l-1}) with gradient G, all contiguous:
+ *   M' = momentum M + G,  U = G + momentum M' (nesterov = 1) or M' (0),
+ *   W' = (1 - eta decay) W - eta sqrt(max(1, rows / cols)) orthogonalised(U).
+ * w_dtype, g_dtype: NF_F32 or NF_BF16 (not bf16 weights with fp32 gradients); the
+ * momentum is fp32.  The orthogonalisation is w_dtype's.  d_w_out may be d_w and
+ * d_m_out may be d_m; no other arrays may share bytes with d_m_out.
+ * d_work: nf_orthogonalize_work(w_dtype, count, rows, cols) bytes, aligned to 256. */
+nf_status nf_muon_step(const void* d_w, int32_t w_dtype, const float* d_m, const void* d_g,
+                       int32_t g_dtype, int64_t count, int64_t rows, int64_t cols, float eta,
+                       float momentum, int32_t nesterov, float decay, void* d_w_out,
+                       float* d_m_out, void* d_work, int64_t work_bytes, void* stream);
+
+/* Rows in 8-bit integers: scale_i = max_j |x_ij| / 127 and
+ * q_ij = rint(x_ij (127 / max_j |x_ij|)), in fp32.  d_x [rows][cols] of dtype NF_F32,
+ * NF_BF16 or NF_F16; d_q [rows][ld_q], aligned to 16 bytes, ld_q a multiple of 16 and
+ * at least cols (columns up to the next multiple of 16 are set to 0);
+ * d_scale [rows].  A row of zeros has scale 0.  A row with a NaN or an infinity
+ * has scale NaN and q of 0.  cols at most NF_LINEAR_I8_MAX. */
+#define NF_LINEAR_I8_MAX 131071
+#define NF_NO_ACT (-1)
+nf_status nf_quantize_rows(const void* d_x, int32_t dtype, int64_t rows, int64_t cols, int64_t ld,
+                           int8_t* d_q, int64_t ld_q, float* d_scale, void* stream);
+
+/* y_ij = act(x_scale_i w_scale_j (sum over k of xq_ik wq_jk) + b_j), the sum
+ * exact.  d_xq [rows][ld_x] and d_wq [outputs][ld_w] as nf_quantize_rows leaves
+ * them (of the weights, columns past `inputs` up to the next multiple of 16 must
+ * be 0); d_bias [outputs] or NULL; act an nf_act or NF_NO_ACT; d_y
+ * [rows][outputs] of y_dtype NF_F32, NF_BF16 or NF_F16.
+ * nf_linear_i8_dynamic takes the rows d_x [rows][inputs] of x_dtype and
+ * quantises them as nf_quantize_rows does; d_work: nf_linear_i8_work(rows,
+ * inputs) bytes, aligned to 16.  d_y may not share bytes with the rows. */
+nf_status nf_linear_i8(const int8_t* d_xq, int64_t ld_x, const float* d_x_scale,
+                       const int8_t* d_wq, int64_t ld_w, const float* d_w_scale,
+                       const float* d_bias, int32_t act, int64_t rows, int64_t inputs,
+                       int64_t outputs, void* d_y, int32_t y_dtype, int64_t ld_y, void* stream);
+int64_t nf_linear_i8_work(int64_t rows, int64_t inputs);
+nf_status nf_linear_i8_dynamic(const void* d_x, int32_t x_dtype, int64_t ld_x, const int8_t* d_wq,
+                               int64_t ld_w, const float* d_w_scale, const float* d_bias,
+                               int32_t act, int64_t rows, int64_t inputs, int64_t outputs,
+                               void* d_y, int32_t y_dtype, int64_t ld_y, void* d_work,
+                               int64_t work_bytes, void* stream);
 
 /* Message for the last failed call on this thread ("" if none).  The pointer
  * stays valid until the next nf_* call on the same thread. */

@@ -28,6 +28,9 @@ SOURCES = ["nf_api.hip", "nf_kernels.hip", "nf_narrow.hip", "nf_narrow64.hip", "
            "nf_eval.hip", "nf_calib.hip", "nf_skinny.hip",
            "nf_wide256.hip", "nf_wide128.hip", "nf_wide64.hip",
            "nf_params.hip"]
+# the operators on the caller's own arrays, apart from the net's kernels
+OPS = os.path.join(HERE, "csrc_ops")
+OPS_SOURCES = ["nf_logprobs.hip", "nf_orth.hip", "nf_linear_i8.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",
@@ -59,9 +62,10 @@ def _run(cmd, verbose):
 def build(verbose: bool = False) -> str:
     objdir = os.path.join(ROOT, "_build")
     os.makedirs(objdir, exist_ok=True)
-    objs = [os.path.join(objdir, os.path.splitext(src)[0] + ".o") for src in SOURCES]
-    cmds = [[hipcc(), *HIPCC_FLAGS, "-c", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
-             os.path.join(CSRC, src), "-o", obj] for src, obj in zip(SOURCES, objs)]
+    paths = [os.path.join(CSRC, s) for s in SOURCES] + [os.path.join(OPS, s) for s in OPS_SOURCES]
+    objs = [os.path.join(objdir, os.path.splitext(os.path.basename(p))[0] + ".o") for p in paths]
+    cmds = [[hipcc(), *HIPCC_FLAGS, "-c", "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-I", OPS,
+             path, "-o", obj] for path, obj in zip(paths, objs)]
     # one compiler process per source, at most as many as the CPUs this
     # process may use
     workers = max(1, min(len(cmds), len(os.sched_getaffinity(0)), 8))

@@ -1,0 +1,684 @@
+// Log probabilities of given classes, entropies and the largest alternatives of
+// rows of logits, and the gradient of a weighted sum of them.
+//
+// With z = scale x, m = max z, s = sum exp(z - m):
+//   log p_j = (z_j - m) - log s,   H = log s - sum exp(z - m) (z - m) / s,
+//   d(g log p_t + h H)/dx_j = scale (g ([j = t] - p_j) - h p_j (log p_j + H)).
+//
+// What bounds it: the bytes of the logits.  A row is read once into registers
+// where they hold it (up to 256 KB), so that the maximum, the sums, the
+// alternatives and the gradient all come from one read; a longer row is read
+// with a running maximum and sum, and again for each of the others.  Rows of at
+// most 128 classes take 8 to 64 lanes of a wave.
+//
+// Alternatives: ordered(z) is a whole number in z's order, so (ordered(z),
+// ~index) orders by value and then by the lower index, and no two are equal.
+// Each wave finds the n_top-th largest of its lanes' maxima (32 ballots); the
+// largest of these is at most the row's n_top-th largest value, so the values
+// from there on hold all alternatives: they go to LDS (a few tens on logits of
+// some spread) and each counts the larger ones.  More than fit there (rows of
+// equal values) are found by n_top searches for the next largest instead.
+#include "ops_common.h"
+
+namespace nf {
+namespace {
+
+constexpr int TOP_MAX = 64;      // a wave's lanes hold enough maxima for the threshold
+constexpr int TOP_CAP = 1024;    // candidates held in LDS
+constexpr int SMALL_MAX = 128;   // classes of the kernel that shares a wave among rows
+
+template <class T>
+struct LogpArgs {
+  const T* x;
+  int64_t rows, ld, ld_dx;
+  int classes, n_top;
+  float scale;
+  const int64_t* target;         // or null: no row has one
+  const float* g;                // gradient: weights of the log probabilities ...
+  const float* h;                // ... and of the entropies, each or null
+  float* logp;                   // outputs, each or null
+  float* entropy;
+  float* stat;                   // [rows][2]: m, log s
+  int* top_ids;                  // [rows][n_top]
+  float* top_logp;
+  T* dx;
+};
+
+// NaN above all numbers, -0 as 0, and nothing at 0 but places that hold no value
+__device__ __forceinline__ unsigned ordered(float z) {
+  if (z != z) return 0xffffffffu;
+  const unsigned b = __builtin_bit_cast(unsigned, z + 0.0f);
+  return b ^ ((unsigned)((int)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float unordered(unsigned k) {
+  return __builtin_bit_cast(float, k & 0x80000000u ? k ^ 0x80000000u : ~k);
+}
+
+// z = scale x rounded to fp32, the same wherever it is formed (never half of a
+// fused multiply-add: z - m of the largest must be 0)
+template <class T>
+__device__ __forceinline__ float z_of(T x, float scale) {
+#pragma clang fp contract(off)
+  return to_float(x) * scale;
+}
+
+__device__ __forceinline__ float exp_of(float d) {
+  return __builtin_amdgcn_exp2f(d * 1.44269504088896340736f);
+}
+
+// What a row's sums come to.  A row whose classes are all at minus infinity has
+// no probabilities: its log probabilities are minus infinity, its entropy and
+// its gradient 0.  A NaN or an infinity of the other sign makes everything NaN.
+struct RowSums {
+  float m, ln, entropy;
+  bool empty;
+};
+__device__ __forceinline__ RowSums row_sums(float m, float s, float t) {
+  RowSums r;
+  r.empty = s == 0.f;
+  r.m = r.empty ? -__builtin_inff() : m;
+  r.ln = r.empty ? -__builtin_inff() : logf(s);
+  r.entropy = r.empty ? 0.f : r.ln - t / s;
+  return r;
+}
+__device__ __forceinline__ float log_prob(const RowSums& r, float z) {
+  return r.empty ? -__builtin_inff() : (z - r.m) - r.ln;
+}
+
+// one value's place in the gradient, without the target's own share
+struct Slope {
+  float m, ln, g, h, entropy, scale;
+  bool empty;
+  __device__ __forceinline__ float at(float z) const {
+    const float d = z - m, p = exp_of(d - ln);
+    const float lp = p == 0.f ? 0.f : d - ln;       // 0 times the logarithm of 0 is 0
+    return empty ? 0.f : -scale * p * (g + h * (lp + entropy));
+  }
+};
+
+template <class T>
+__device__ __forceinline__ void put_row(const LogpArgs<T>& a, int64_t row, const RowSums& r, int64_t t, float zt) {
+  if (a.logp)
+    a.logp[row] = t < 0 ? 0.f : t >= a.classes ? __builtin_nanf("") : log_prob(r, zt);
+  if (a.entropy) a.entropy[row] = r.entropy;
+  if (a.stat) {
+    a.stat[2 * row] = r.m;
+    a.stat[2 * row + 1] = r.ln;
+  }
+}
+
+template <class T>
+__device__ __forceinline__ Slope slope_of(const LogpArgs<T>& a, int64_t row, const RowSums& r, int64_t t) {
+  Slope s;
+  s.m = r.m;
+  s.ln = r.ln;
+  // a row without a target has no log probability to change; a target past the
+  // classes leaves no gradient that could be taken for one
+  s.g = t < 0 || !a.g ? 0.f : t >= a.classes ? __builtin_nanf("") : a.g[row];
+  s.h = a.h ? a.h[row] : 0.f;
+  s.entropy = r.entropy;
+  s.scale = a.scale;
+  s.empty = r.empty && t < a.classes;
+  return s;
+}
+
+// ---- rows of at most SMALL_MAX classes: G lanes a row, two values a lane -----
+template <class T, int G, bool GRAD>
+__global__ void __launch_bounds__(256) logp_small_kernel(const LogpArgs<T> a) {
+  const int lane = threadIdx.x & 63, at = lane & (G - 1);
+  const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / G;
+  const bool live = row < a.rows;
+  const int64_t r0 = live ? row : a.rows - 1;
+  const T* const x = a.x + r0 * a.ld;
+  const int64_t t = a.target ? a.target[r0] : -1;
+  float z[2];
+  bool in[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int j = at + e * G;
+    in[e] = j < a.classes;
+    z[e] = in[e] ? z_of(x[j], a.scale) : -__builtin_inff();
+  }
+  float m = fmaxf(z[0], z[1]);
+#pragma unroll
+  for (int o = G / 2; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  const float mm = m == -__builtin_inff() ? 0.f : m;
+  float s = 0.f, q = 0.f;
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const float d = z[e] - mm, w = exp_of(d);
+    s += w;
+    q += w == 0.f ? 0.f : w * d;
+  }
+#pragma unroll
+  for (int o = G / 2; o >= 1; o >>= 1) {
+    s += __shfl_xor(s, o, 64);
+    q += __shfl_xor(q, o, 64);
+  }
+  const RowSums r = row_sums(mm, s, q);
+  if (live && at == 0) put_row(a, row, r, t, t >= 0 && t < a.classes ? z_of(x[t], a.scale) : 0.f);
+  if (a.n_top > 0) {
+    unsigned k[2];
+    int rank[2] = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 2; ++e) k[e] = in[e] ? ordered(z[e]) : 0u;
+    for (int c = 0; c < G; ++c) {
+#pragma unroll
+      for (int f = 0; f < 2; ++f) {
+        const unsigned other = __shfl(k[f], c, G);
+        const int oj = c + f * G;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          rank[e] += other > k[e] || (other == k[e] && oj < at + e * G);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      if (live && in[e] && rank[e] < a.n_top) {
+        const int64_t o = row * a.n_top + rank[e];
+        if (a.top_ids) a.top_ids[o] = at + e * G;
+        if (a.top_logp) a.top_logp[o] = log_prob(r, z[e]);
+      }
+  }
+  if constexpr (GRAD) {
+    const Slope sl = slope_of(a, r0, r, t);
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      if (live && in[e]) {
+        const int j = at + e * G;
+        const float own = j == t && !sl.empty ? sl.scale * sl.g : 0.f;
+        a.dx[row * a.ld_dx + j] = from_float<T>(sl.at(z[e]) + own);
+      }
+  }
+}
+
+// ---- longer rows: one workgroup each ----------------------------------------
+template <int W>
+struct BlockShare {
+  float m[W], s[W], q[W];
+  unsigned top[W];
+  float zt;
+  int count;
+  unsigned long long best[W];
+  unsigned long long key[TOP_CAP];
+};
+
+// NV: 16-byte vectors of the row that a thread holds; 0: none, the row is read
+// anew for each pass over it
+template <class T, int THREADS, int NV, bool GRAD>
+__global__ void __launch_bounds__(THREADS) logp_row_kernel(const LogpArgs<T> a) {
+  constexpr int E = Vec16<T>::N, W = THREADS / 64;
+  __shared__ BlockShare<W> sh;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t row = blockIdx.x;
+  const T* const x = a.x + row * a.ld;
+  const int V = a.classes;
+
+  auto load = [&](int j) {           // E values from class j on, minus infinity past the last
+    if (j + E <= V) return load16(x + j);
+    Vec16<T> r;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      r.v[e] = from_float<T>(-__builtin_inff());
+      if (j + e < V) r.v[e] = x[j + e];
+    }
+    return r;
+  };
+  Vec16<T> keep[NV > 0 ? NV : 1];
+  if constexpr (NV > 0) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) keep[v] = load((v * THREADS + tid) * E);
+  }
+  // f(j, vector): each of the thread's vectors that begins inside the row
+  auto each = [&](auto&& f) {
+    if constexpr (NV > 0) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int j = (v * THREADS + tid) * E;
+        if (j < V) f(j, keep[v]);
+      }
+    } else {
+      constexpr int U = 4;
+      int j = tid * E;
+      for (; j + (U - 1) * THREADS * E < V; j += U * THREADS * E) {
+        Vec16<T> r[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) r[u] = load(j + u * THREADS * E);
+#pragma unroll
+        for (int u = 0; u < U; ++u) f(j + u * THREADS * E, r[u]);
+      }
+      for (; j < V; j += THREADS * E) f(j, load(j));
+    }
+  };
+  const int64_t t = a.target ? a.target[row] : -1;
+  float zt = 0.f;
+  if (tid == 0 && t >= 0 && t < V) zt = z_of(x[t], a.scale);
+
+  // maximum and sums
+  float m = -__builtin_inff(), s = 0.f, q = 0.f;
+  auto add = [&](const Vec16<T>& r, float mm) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const float d = z_of(r.v[e], a.scale) - mm, w = exp_of(d);
+      s += w;
+      q += w == 0.f ? 0.f : w * d;
+    }
+  };
+  if constexpr (NV > 0) {
+    each([&](int, const Vec16<T>& r) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) m = fmaxf(m, z_of(r.v[e], a.scale));
+    });
+    m = wave_max(m);
+    if constexpr (W > 1) {
+      if (lane == 0) sh.m[wave] = m;
+      __syncthreads();
+      m = sh.m[0];
+#pragma unroll
+      for (int w = 1; w < W; ++w) m = fmaxf(m, sh.m[w]);
+    }
+    m = m == -__builtin_inff() ? 0.f : m;
+    each([&](int, const Vec16<T>& r) { add(r, m); });
+  } else {
+    // running: the sums are relative to the thread's maximum so far
+    float run = -__builtin_inff();
+    m = 0.f;
+    each([&](int, const Vec16<T>& r) {
+      float c = run;
+#pragma unroll
+      for (int e = 0; e < E; ++e) c = fmaxf(c, z_of(r.v[e], a.scale));
+      if (c > run) {
+        const float d = run - c, w = exp_of(d);       // run may be minus infinity: s is 0 then
+        q = w == 0.f ? 0.f : w * (q + s * d);
+        s *= w;
+        run = m = c;
+      }
+      add(r, m);
+    });
+    const float own = run;
+    m = wave_max(run);
+    if (lane == 0) sh.m[wave] = m;
+    __syncthreads();
+    m = sh.m[0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) m = fmaxf(m, sh.m[w]);
+    m = m == -__builtin_inff() ? 0.f : m;
+    const float d = own - m, w = exp_of(d);
+    // a thread without a finite value may still hold a NaN
+    if (own != -__builtin_inff()) {
+      q = w == 0.f ? 0.f * q : w * (q + s * d);
+      s *= w;
+    }
+  }
+  s = wave_sum(s);
+  q = wave_sum(q);
+  if constexpr (W > 1) {
+    if (lane == 0) {
+      sh.s[wave] = s;
+      sh.q[wave] = q;
+    }
+    if (tid == 0) sh.count = 0;
+    __syncthreads();
+    s = q = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      s += sh.s[w];
+      q += sh.q[w];
+    }
+  } else {
+    if (tid == 0) sh.count = 0;
+  }
+  const RowSums r = row_sums(m, s, q);
+  if (tid == 0) put_row(a, row, r, t, zt);
+
+  if constexpr (GRAD) {
+    const Slope sl = slope_of(a, row, r, t);
+    T* const dx = a.dx + row * a.ld_dx;
+    const float own = sl.empty ? 0.f : sl.scale * sl.g;
+    each([&](int j, const Vec16<T>& v) {
+      Vec16<T> o;
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        o.v[e] = from_float<T>(sl.at(z_of(v.v[e], a.scale)) + (j + e == t ? own : 0.f));
+      if (j + E <= V) {
+        store16(dx + j, o);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (j + e < V) dx[j + e] = o.v[e];
+      }
+    });
+    return;
+  }
+  if (a.n_top <= 0) return;
+
+  // the largest of the waves' n_top-th largest lane maxima
+  unsigned most = 0;
+  each([&](int j, const Vec16<T>& v) {
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (j + e < V) most = max(most, ordered(z_of(v.v[e], a.scale)));
+  });
+  unsigned from = 0;
+#pragma unroll
+  for (int b = 31; b >= 0; --b) {
+    const unsigned c = from | (1u << b);
+    if (__popcll(__ballot(most >= c)) >= a.n_top) from = c;
+  }
+  if constexpr (W > 1) {
+    if (lane == 0) sh.top[wave] = from;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) from = max(from, sh.top[w]);
+  } else {
+    __syncthreads();
+  }
+  from = max(from, 1u);
+  if (most >= from)
+    each([&](int j, const Vec16<T>& v) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const unsigned k = j + e < V ? ordered(z_of(v.v[e], a.scale)) : 0u;
+        if (k >= from) {
+          const int at = atomicAdd(&sh.count, 1);
+          if (at < TOP_CAP) sh.key[at] = (unsigned long long)k << 32 | (unsigned)~(unsigned)(j + e);
+        }
+      }
+    });
+  __syncthreads();
+  const int n = sh.count;
+  auto put = [&](int rank, unsigned long long key) {
+    const int64_t o = row * a.n_top + rank;
+    if (a.top_ids) a.top_ids[o] = (int)~(unsigned)key;
+    if (a.top_logp) a.top_logp[o] = log_prob(r, unordered((unsigned)(key >> 32)));
+  };
+  if (n <= TOP_CAP) {
+    for (int c = tid; c < n; c += THREADS) {
+      const unsigned long long key = sh.key[c];
+      int rank = 0;
+      for (int o = 0; o < n; ++o) rank += sh.key[o] > key;
+      if (rank < a.n_top) put(rank, key);
+    }
+    return;
+  }
+  unsigned long long last = ~0ull;      // above every key: the lowest index of a NaN has a smaller one
+  for (int k = 0; k < a.n_top; ++k) {
+    unsigned long long best = 0;
+    each([&](int j, const Vec16<T>& v) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const unsigned o = j + e < V ? ordered(z_of(v.v[e], a.scale)) : 0u;
+        const unsigned long long key = (unsigned long long)o << 32 | (unsigned)~(unsigned)(j + e);
+        if (o && (k == 0 || key < last) && key > best) best = key;
+      }
+    });
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) {
+      const unsigned long long other = __shfl_xor(best, o, 64);
+      best = other > best ? other : best;
+    }
+    if (lane == 0) sh.best[wave] = best;
+    __syncthreads();
+    best = sh.best[0];
+    for (int w = 1; w < W; ++w) best = sh.best[w] > best ? sh.best[w] : best;
+    __syncthreads();
+    last = best;
+    if (tid == 0) put(k, best);
+  }
+}
+
+// ---- the gradient from statistics kept earlier ------------------------------
+template <class T>
+struct GradArgs {
+  const T* x;
+  T* dx;
+  int64_t ld, ld_dx;
+  int64_t rows, blocks;            // blocks of vectors in all
+  int classes, per_row;            // workgroups a row
+  float scale;
+  const int64_t* target;
+  const float* stat;
+  const float* entropy;
+  const float* g;
+  const float* h;
+};
+
+constexpr int GRAD_VECS = 4;
+
+template <class T>
+__global__ void __launch_bounds__(256) logp_grad_kernel(const GradArgs<T> a) {
+  constexpr int E = Vec16<T>::N;
+  const int64_t row = blockIdx.x / a.per_row;
+  const int first = (int)(blockIdx.x - row * a.per_row) * 256 * E * GRAD_VECS;
+  const int V = a.classes;
+  const T* const x = a.x + row * a.ld;
+  T* const dx = a.dx + row * a.ld_dx;
+  Vec16<T> v[GRAD_VECS];
+#pragma unroll
+  for (int u = 0; u < GRAD_VECS; ++u) {
+    const int j = first + (u * 256 + (int)threadIdx.x) * E;
+    if (j + E <= V) {
+      v[u] = load16(x + j);
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        v[u].v[e] = from_float<T>(0.f);
+        if (j + e < V) v[u].v[e] = x[j + e];
+      }
+    }
+  }
+  const int64_t t = a.target ? a.target[row] : -1;
+  Slope sl;
+  sl.m = a.stat[2 * row];
+  sl.ln = a.stat[2 * row + 1];
+  sl.g = t < 0 || !a.g ? 0.f : t >= V ? __builtin_nanf("") : a.g[row];
+  sl.h = a.h ? a.h[row] : 0.f;
+  sl.entropy = a.h ? a.entropy[row] : 0.f;
+  sl.scale = a.scale;
+  sl.empty = sl.ln == -__builtin_inff() && t < V;
+  const float own = sl.empty ? 0.f : sl.scale * sl.g;
+#pragma unroll
+  for (int u = 0; u < GRAD_VECS; ++u) {
+    const int j = first + (u * 256 + (int)threadIdx.x) * E;
+    Vec16<T> o;
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      o.v[e] = from_float<T>(sl.at(z_of(v[u].v[e], a.scale)) + (j + e == t ? own : 0.f));
+    if (j + E <= V) {
+      store16(dx + j, o);
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (j + e < V) dx[j + e] = o.v[e];
+    }
+  }
+}
+
+// ---- launches ----------------------------------------------------------------
+template <class T, bool GRAD>
+hipError_t launch_logp(const LogpArgs<T>& a, hipStream_t s) {
+  if (a.classes <= SMALL_MAX) {
+    const int half = (a.classes + 1) / 2;
+    auto go = [&](auto g) {
+      constexpr int G = decltype(g)::value;
+      const int64_t blocks = (a.rows + 256 / G - 1) / (256 / G);
+      return launch_k(logp_small_kernel<T, G, GRAD>, dim3((unsigned)blocks), dim3(256), 0, s, a);
+    };
+    if (half <= 8) return go(std::integral_constant<int, 8>());
+    if (half <= 16) return go(std::integral_constant<int, 16>());
+    if (half <= 32) return go(std::integral_constant<int, 32>());
+    return go(std::integral_constant<int, 64>());
+  }
+  const int64_t vecs = (a.classes + Vec16<T>::N - 1) / Vec16<T>::N;
+#define NF_ROW(TH, NV) \
+  if (vecs <= (int64_t)(TH) * (NV))  \
+    return launch_k(logp_row_kernel<T, TH, NV, GRAD>, dim3((unsigned)a.rows), dim3(TH), 0, s, a);
+  NF_ROW(64, 1)
+  NF_ROW(64, 4)
+  NF_ROW(256, 2)
+  NF_ROW(256, 4)
+  NF_ROW(256, 8)
+  NF_ROW(1024, 4)
+  NF_ROW(1024, 8)
+  NF_ROW(1024, 16)
+#undef NF_ROW
+  return launch_k(logp_row_kernel<T, 1024, 0, GRAD>, dim3((unsigned)a.rows), dim3(1024), 0, s, a);
+}
+
+nf_status check_logits(const void* x, int dtype, int64_t rows, int64_t classes, int64_t ld, float scale) {
+  if (!op_float_type(dtype)) return op_fail(NF_EINVAL, "logits must be fp32, bf16 or fp16 (dtype %d)", dtype);
+  if (rows < 0 || classes < 1) return op_fail(NF_EINVAL, "rows must be at least 0, classes at least 1");
+  if (rows > 0x7fffffff || classes > (1 << 30))
+    return op_fail(NF_ESHAPE, "at most 2^31 - 1 rows of 2^30 classes");
+  if (ld < classes) return op_fail(NF_ESHAPE, "the row pitch is smaller than the classes");
+  if (rows > 0 && ld > INT64_MAX / 4 / rows) return op_fail(NF_ESHAPE, "rows times pitch does not fit");
+  if (!(scale > 0.f && scale < __builtin_inff())) return op_fail(NF_EINVAL, "scale must be positive and finite");
+  if (rows > 0 && !x) return op_fail(NF_EINVAL, "NULL logits");
+  if (!op_aligned(x, (uintptr_t)op_size(dtype))) return op_fail(NF_EINVAL, "logits are not aligned to their elements");
+  return NF_OK;
+}
+
+// The gradient may be written over the logits themselves, and over nothing else
+// that the call reads.
+nf_status check_gradient(const void* x, int64_t ld, const void* dx, int64_t ld_dx, int dtype, int64_t rows,
+                         int64_t classes) {
+  if (!dx) return op_fail(NF_EINVAL, "NULL gradient");
+  if (ld_dx < classes) return op_fail(NF_ESHAPE, "the gradient's row pitch is smaller than the classes");
+  if (ld_dx > INT64_MAX / 4 / rows) return op_fail(NF_ESHAPE, "rows times pitch does not fit");
+  if (!op_aligned(dx, (uintptr_t)op_size(dtype))) return op_fail(NF_EINVAL, "the gradient is not aligned to its elements");
+  const int64_t e = op_size(dtype);
+  if (!(x == dx && ld == ld_dx) &&
+      op_overlap(x, ((rows - 1) * ld + classes) * e, dx, ((rows - 1) * ld_dx + classes) * e))
+    return op_fail(NF_EINVAL, "the gradient overlaps the logits without being them");
+  return NF_OK;
+}
+
+}  // namespace
+
+int op_compute_units() {
+  thread_local int at = -1, units = 0;
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess) {
+    (void)hipGetLastError();
+    return 0;
+  }
+  if (dev != at) {
+    int n = 0;
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) {
+      (void)hipGetLastError();
+      return 0;
+    }
+    at = dev;
+    units = n;
+  }
+  return units;
+}
+
+}  // namespace nf
+
+using namespace nf;
+
+extern "C" {
+
+nf_status nf_logprobs(const void* d_logits, int32_t dtype, int64_t rows, int64_t classes, int64_t ld, float scale,
+                      const int64_t* d_targets, int32_t n_top, float* d_logp, float* d_entropy, float* d_stat,
+                      int32_t* d_top_ids, float* d_top_logp, void* stream) {
+  op_begin();
+  const nf_status st = check_logits(d_logits, dtype, rows, classes, ld, scale);
+  if (st != NF_OK) return st;
+  if (n_top < 0 || n_top > NF_TOP_MAX) return op_fail(NF_EINVAL, "n_top must be in 0 .. %d", NF_TOP_MAX);
+  if (n_top > classes) return op_fail(NF_ESHAPE, "more alternatives than classes");
+  if (n_top > 0 && !d_top_ids && !d_top_logp) return op_fail(NF_EINVAL, "alternatives without a place for them");
+  if (rows == 0) return NF_OK;
+  if (op_compute_units() <= 0) return op_fail(NF_EDEVICE, "no usable HIP device");
+  return with_type(dtype, [&](auto e) {
+    typedef decltype(e) T;
+    LogpArgs<T> a{};
+    a.x = static_cast<const T*>(d_logits);
+    a.rows = rows;
+    a.ld = ld;
+    a.classes = (int)classes;
+    a.n_top = n_top;
+    a.scale = scale;
+    a.target = d_targets;
+    a.logp = d_logp;
+    a.entropy = d_entropy;
+    a.stat = d_stat;
+    a.top_ids = d_top_ids;
+    a.top_logp = d_top_logp;
+    return op_result(launch_logp<T, false>(a, static_cast<hipStream_t>(stream)), "log probabilities");
+  });
+}
+
+nf_status nf_logprobs_train(const void* d_logits, int32_t dtype, int64_t rows, int64_t classes, int64_t ld,
+                            float scale, const int64_t* d_targets, const float* d_g_logp, const float* d_g_entropy,
+                            float* d_logp, float* d_entropy, float* d_stat, void* d_dlogits, int64_t ld_d,
+                            void* stream) {
+  op_begin();
+  nf_status st = check_logits(d_logits, dtype, rows, classes, ld, scale);
+  if (st != NF_OK) return st;
+  if (rows == 0) return NF_OK;
+  if (d_g_logp && !d_targets) return op_fail(NF_EINVAL, "weights of log probabilities without targets");
+  st = check_gradient(d_logits, ld, d_dlogits, ld_d, dtype, rows, classes);
+  if (st != NF_OK) return st;
+  if (op_compute_units() <= 0) return op_fail(NF_EDEVICE, "no usable HIP device");
+  return with_type(dtype, [&](auto e) {
+    typedef decltype(e) T;
+    LogpArgs<T> a{};
+    a.x = static_cast<const T*>(d_logits);
+    a.rows = rows;
+    a.ld = ld;
+    a.ld_dx = ld_d;
+    a.classes = (int)classes;
+    a.scale = scale;
+    a.target = d_targets;
+    a.g = d_g_logp;
+    a.h = d_g_entropy;
+    a.logp = d_logp;
+    a.entropy = d_entropy;
+    a.stat = d_stat;
+    a.dx = static_cast<T*>(d_dlogits);
+    return op_result(launch_logp<T, true>(a, static_cast<hipStream_t>(stream)), "log probabilities and gradient");
+  });
+}
+
+nf_status nf_logprobs_grad(const void* d_logits, int32_t dtype, int64_t rows, int64_t classes, int64_t ld,
+                           float scale, const int64_t* d_targets, const float* d_stat, const float* d_entropy,
+                           const float* d_g_logp, const float* d_g_entropy, void* d_dlogits, int64_t ld_d,
+                           void* stream) {
+  op_begin();
+  nf_status st = check_logits(d_logits, dtype, rows, classes, ld, scale);
+  if (st != NF_OK) return st;
+  if (rows == 0) return NF_OK;
+  if (!d_stat) return op_fail(NF_EINVAL, "NULL statistics");
+  if (d_g_logp && !d_targets) return op_fail(NF_EINVAL, "weights of log probabilities without targets");
+  if (d_g_entropy && !d_entropy) return op_fail(NF_EINVAL, "weights of entropies without the entropies");
+  st = check_gradient(d_logits, ld, d_dlogits, ld_d, dtype, rows, classes);
+  if (st != NF_OK) return st;
+  if (op_compute_units() <= 0) return op_fail(NF_EDEVICE, "no usable HIP device");
+  return with_type(dtype, [&](auto e) {
+    typedef decltype(e) T;
+    GradArgs<T> a{};
+    a.x = static_cast<const T*>(d_logits);
+    a.dx = static_cast<T*>(d_dlogits);
+    a.ld = ld;
+    a.ld_dx = ld_d;
+    a.rows = rows;
+    a.classes = (int)classes;
+    constexpr int64_t per = 256 * Vec16<T>::N * GRAD_VECS;
+    a.per_row = (int)((classes + per - 1) / per);
+    a.blocks = rows * a.per_row;
+    if (a.blocks > 0x7fffffff) return op_fail(NF_ESHAPE, "too many logits for one call");
+    a.scale = scale;
+    a.target = d_targets;
+    a.stat = d_stat;
+    a.entropy = d_entropy;
+    a.g = d_g_logp;
+    a.h = d_g_entropy;
+    return op_result(launch_k(logp_grad_kernel<T>, dim3((unsigned)a.blocks), dim3(256), 0,
+                              static_cast<hipStream_t>(stream), a),
+                     "gradient of log probabilities");
+  });
+}
+
+}  // extern "C"

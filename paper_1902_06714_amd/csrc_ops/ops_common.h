@@ -1,0 +1,135 @@
+// What the operators for the last layers of a language model share: element
+// types, loads of rows at any alignment, reductions, and the checks that every
+// entry point makes before it enqueues anything.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <cstdio>
+#include <type_traits>
+
+#include "nf.h"
+#include "nf_internal.h"
+
+namespace nf {
+
+struct bf16_t {
+  uint16_t bits;
+};
+struct f16_t {
+  _Float16 v;
+};
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(bf16_t x) {
+  return __builtin_bit_cast(float, (unsigned)x.bits << 16);
+}
+__device__ __forceinline__ float to_float(f16_t x) { return (float)x.v; }
+
+// rounded to nearest, ties to even (NaN stays NaN)
+template <class T>
+__device__ __forceinline__ T from_float(float x) {
+  if constexpr (std::is_same_v<T, float>) {
+    return x;
+  } else if constexpr (std::is_same_v<T, bf16_t>) {
+    return {__builtin_bit_cast(uint16_t, (__bf16)x)};
+  } else {
+    return {(_Float16)x};
+  }
+}
+
+template <class T>
+constexpr unsigned neg_inf_bits() {
+  return std::is_same_v<T, float> ? 0xff800000u : std::is_same_v<T, bf16_t> ? 0xff80u : 0xfc00u;
+}
+
+// 16 bytes of a row, at any address that its elements may have (the hardware
+// takes wide loads and stores at any alignment)
+template <class T>
+struct Vec16 {
+  static constexpr int N = 16 / sizeof(T);
+  T v[N];
+};
+template <class T>
+__device__ __forceinline__ Vec16<T> load16(const T* p) {
+  Vec16<T> r;
+  __builtin_memcpy(&r, p, 16);
+  return r;
+}
+template <class T>
+__device__ __forceinline__ void store16(T* p, const Vec16<T>& r) {
+  __builtin_memcpy(p, &r, 16);
+}
+
+// Sums and maxima over a wave, in a fixed order; every lane gets the result.
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o, 64);
+  return x;
+}
+__device__ __forceinline__ double wave_sum(double x) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o, 64);
+  return x;
+}
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
+  return x;
+}
+
+// ---- entry points ----------------------------------------------------------
+// The message is formatted into a fixed buffer; no exception leaves an entry.
+template <class... A>
+nf_status op_fail(nf_status st, const char* fmt, A... a) {
+  char msg[256];
+  std::snprintf(msg, sizeof msg, fmt, a...);
+  try {
+    set_error_message(msg);
+  } catch (...) {
+  }
+  return st;
+}
+inline nf_status op_fail(nf_status st, const char* msg) {
+  try {
+    set_error_message(msg);
+  } catch (...) {
+  }
+  return st;
+}
+inline void op_begin() {
+  try {
+    set_error_message("");
+  } catch (...) {
+  }
+}
+inline nf_status op_result(hipError_t e, const char* what) {
+  if (e == hipSuccess) return NF_OK;
+  (void)hipGetLastError();
+  return op_fail(NF_EDEVICE, "%s: %s", what, hipGetErrorString(e));
+}
+
+// Compute units of the current device, or 0 where there is none (asked once
+// for each device).
+int op_compute_units();
+
+inline bool op_float_type(int dtype) { return dtype == NF_F32 || dtype == NF_BF16 || dtype == NF_F16; }
+inline int64_t op_size(int dtype) { return dtype == NF_F32 ? 4 : 2; }
+inline bool op_aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+// Whether two ranges of bytes share any.
+inline bool op_overlap(const void* a, int64_t na, const void* b, int64_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && na > 0 && nb > 0 && x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
+}
+
+// Calls f with a value of the element type `dtype` names.
+template <class F>
+auto with_type(int dtype, F&& f) {
+  if (dtype == NF_BF16) return f(bf16_t());
+  if (dtype == NF_F16) return f(f16_t());
+  return f(float());
+}
+
+}  // namespace nf

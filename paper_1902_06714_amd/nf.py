@@ -40,7 +40,7 @@ NF_GAUSSIAN, NF_RELU, NF_SIGMOID, NF_STEP, NF_TANH = 0, 1, 2, 3, 4
 ACT_CODES = {"gaussian": NF_GAUSSIAN, "relu": NF_RELU, "sigmoid": NF_SIGMOID,
              "step": NF_STEP, "tanh": NF_TANH}
 NF_OK, NF_EINVAL, NF_ESHAPE, NF_ENOMEM, NF_EDEVICE = 0, -1, -2, -3, -4
-NF_F32, NF_F64 = 0, 1
+NF_F32, NF_F64, NF_BF16, NF_F16 = 0, 1, 2, 3
 STATUS_NAMES = {0: "NF_OK", -1: "NF_EINVAL", -2: "NF_ESHAPE", -3: "NF_ENOMEM", -4: "NF_EDEVICE"}
 
 _c_i32p = ctypes.POINTER(ctypes.c_int32)
@@ -120,6 +120,25 @@ _sig = {
     "nf_calib_spin": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_double]),
     "nf_last_error": (ctypes.c_char_p, []),
 }
+_p, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+_sig.update({
+    "nf_logprobs": (ctypes.c_int, [_p, _i32, _i64, _i64, _i64, _f32, _p, _i32, _p, _p, _p, _p, _p, _p]),
+    "nf_logprobs_train": (ctypes.c_int, [_p, _i32, _i64, _i64, _i64, _f32, _p, _p, _p, _p, _p, _p,
+                                         _p, _i64, _p]),
+    "nf_logprobs_grad": (ctypes.c_int, [_p, _i32, _i64, _i64, _i64, _f32, _p, _p, _p, _p, _p, _p,
+                                        _i64, _p]),
+    "nf_orthogonalize_work": (_i64, [_i32, _i64, _i64, _i64]),
+    "nf_orthogonalize": (ctypes.c_int, [_p, _i32, _i64, _i64, _i64, _i64, _i64, _p, _i64, _i64, _p,
+                                        _i64, _p]),
+    "nf_muon_step": (ctypes.c_int, [_p, _i32, _p, _p, _i32, _i64, _i64, _i64, _f32, _f32, _i32,
+                                    _f32, _p, _p, _p, _i64, _p]),
+    "nf_quantize_rows": (ctypes.c_int, [_p, _i32, _i64, _i64, _i64, _p, _i64, _p, _p]),
+    "nf_linear_i8": (ctypes.c_int, [_p, _i64, _p, _p, _i64, _p, _p, _i32, _i64, _i64, _i64, _p,
+                                    _i32, _i64, _p]),
+    "nf_linear_i8_work": (_i64, [_i64, _i64]),
+    "nf_linear_i8_dynamic": (ctypes.c_int, [_p, _i32, _i64, _p, _i64, _p, _p, _i32, _i64, _i64, _i64,
+                                            _p, _i32, _i64, _p, _i64, _p]),
+})
 for _name, (_res, _args) in _sig.items():
     _fn = getattr(_lib, _name)
     _fn.restype = _res
@@ -393,6 +412,245 @@ def nf_calib_mfma(dtype: int, iters: int, sink, stream=None):
 def nf_calib_spin(us: float, stream=None) -> None:
     """Hold the stream for `us` microseconds (returns at once)."""
     _check(_lib.nf_calib_spin(_stream(stream), float(us)), "nf_calib_spin")
+
+
+# -- operators on the caller's own tensors ------------------------------------
+# Matrices are 2-D (stacks 3-D) GPU tensors whose rows are contiguous; vectors
+# are contiguous.  Outputs are the caller's tensors; None leaves one out.
+NF_TOP_MAX, NF_ORTH_MAX, NF_ORTH_STEPS, NF_LINEAR_I8_MAX, NF_NO_ACT = 64, 65536, 5, 131071, -1
+_elems = {}
+
+
+def _elem(t, name: str) -> int:
+    """nf_dtype of a GPU tensor on the current device."""
+    import torch
+    if not _elems:
+        _elems.update({torch.float32: NF_F32, torch.bfloat16: NF_BF16, torch.float16: NF_F16})
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor on the GPU")
+    code = _elems.get(t.dtype)
+    if code is None or not t.is_cuda:
+        raise ValueError(f"{name} must be an fp32, bf16 or fp16 GPU tensor")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} is not on the current device")
+    return code
+
+
+def _matrix(t, name: str, shape=None):
+    """(pointer, rows, columns, row pitch) of a 2-D tensor of contiguous rows."""
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
+        raise ValueError(f"{name} must be 2-D" + (f" of shape {shape}" if shape else ""))
+    rows, cols = t.shape
+    ld, one = t.stride()
+    if rows <= 1:
+        ld = cols
+    if (one != 1 and cols > 1) or ld < cols:
+        raise ValueError(f"{name}'s rows must be contiguous and apart")
+    return t.data_ptr(), rows, cols, ld
+
+
+def _vector(t, name: str, dtype, shape):
+    """Pointer of a contiguous GPU tensor of this type and shape, None for None."""
+    if t is None:
+        return None
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor on the GPU")
+    if t.dtype != dtype or not t.is_cuda or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} GPU tensor of shape {shape}")
+    return t.data_ptr()
+
+
+def _queue(stream):
+    if stream is not None:
+        return _stream(stream)
+    import torch
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None
+
+
+def _workspace(work, need: int, stream, name: str):
+    """(pointer, bytes, tensor) of the caller's workspace, or of one from torch's
+    allocator, which keeps it until the stream has passed the call."""
+    import torch
+    if need < 0:
+        raise NfError(NF_ESHAPE, name)
+    if work is None:
+        work = torch.empty(need, dtype=torch.uint8, device="cuda")
+        if stream is not None:
+            work.record_stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
+    elif not isinstance(work, torch.Tensor) or not work.is_cuda or not work.is_contiguous():
+        raise ValueError("work must be a contiguous GPU tensor")
+    return work.data_ptr(), work.numel() * work.element_size(), work
+
+
+def nf_logprobs(logits, targets=None, logp=None, entropy=None, stat=None, top_ids=None, top_logp=None,
+                scale: float = 1.0, stream=None) -> None:
+    """logits [rows][classes], targets [rows] int64; logp, entropy [rows], stat
+    [rows][2], top_ids (int32) and top_logp [rows][n_top] receive what they name."""
+    import torch
+    code = _elem(logits, "logits")
+    x, rows, cols, ld = _matrix(logits, "logits")
+    f = torch.float32
+    top = top_ids if top_ids is not None else top_logp
+    n_top = 0 if top is None else top.shape[-1]
+    _check(_lib.nf_logprobs(x, code, rows, cols, ld, scale, _vector(targets, "targets", torch.int64, (rows,)),
+                            n_top, _vector(logp, "logp", f, (rows,)), _vector(entropy, "entropy", f, (rows,)),
+                            _vector(stat, "stat", f, (rows, 2)),
+                            _vector(top_ids, "top_ids", torch.int32, (rows, n_top)),
+                            _vector(top_logp, "top_logp", f, (rows, n_top)), _queue(stream)), "nf_logprobs")
+
+
+def _like(t, of, code: int, name: str):
+    if _elem(t, name) != code:
+        raise ValueError(f"{name} must have the type of the logits")
+    p, _, _, ld = _matrix(t, name, tuple(of.shape))
+    return p, ld
+
+
+def nf_logprobs_train(logits, targets, g_logp, g_entropy, dlogits, logp=None, entropy=None, stat=None,
+                      scale: float = 1.0, stream=None) -> None:
+    """nf_logprobs with the gradient of sum(g_logp logp + g_entropy entropy) in
+    dlogits [rows][classes], which may be the logits."""
+    import torch
+    code = _elem(logits, "logits")
+    x, rows, cols, ld = _matrix(logits, "logits")
+    dx, ldd = _like(dlogits, logits, code, "dlogits")
+    f = torch.float32
+    _check(_lib.nf_logprobs_train(x, code, rows, cols, ld, scale, _vector(targets, "targets", torch.int64, (rows,)),
+                                  _vector(g_logp, "g_logp", f, (rows,)),
+                                  _vector(g_entropy, "g_entropy", f, (rows,)), _vector(logp, "logp", f, (rows,)),
+                                  _vector(entropy, "entropy", f, (rows,)), _vector(stat, "stat", f, (rows, 2)),
+                                  dx, ldd, _queue(stream)), "nf_logprobs_train")
+
+
+def nf_logprobs_grad(logits, targets, stat, entropy, g_logp, g_entropy, dlogits, scale: float = 1.0,
+                     stream=None) -> None:
+    """The same gradient from the stat (and entropy) of an earlier nf_logprobs."""
+    import torch
+    code = _elem(logits, "logits")
+    x, rows, cols, ld = _matrix(logits, "logits")
+    dx, ldd = _like(dlogits, logits, code, "dlogits")
+    f = torch.float32
+    _check(_lib.nf_logprobs_grad(x, code, rows, cols, ld, scale, _vector(targets, "targets", torch.int64, (rows,)),
+                                 _vector(stat, "stat", f, (rows, 2)), _vector(entropy, "entropy", f, (rows,)),
+                                 _vector(g_logp, "g_logp", f, (rows,)),
+                                 _vector(g_entropy, "g_entropy", f, (rows,)), dx, ldd, _queue(stream)),
+           "nf_logprobs_grad")
+
+
+def _stack(t, name: str):
+    """(pointer, count, rows, columns, row pitch, matrix pitch) of a matrix or a stack."""
+    if t.dim() not in (2, 3):
+        raise ValueError(f"{name} must be a matrix or a stack of matrices")
+    count = t.shape[0] if t.dim() == 3 else 1
+    stride = t.stride(0) if t.dim() == 3 and count > 1 else 0
+    rows, cols = t.shape[-2:]
+    ld, one = t.stride()[-2:]
+    if rows <= 1:
+        ld = cols
+    if (one != 1 and cols > 1) or ld < cols:
+        raise ValueError(f"{name}'s rows must be contiguous and apart")
+    return t.data_ptr(), count, rows, cols, ld, stride
+
+
+def nf_orthogonalize_work(dtype: int, count: int, rows: int, cols: int) -> int:
+    """Bytes of workspace; raises for sizes that nf_orthogonalize would refuse."""
+    n = _lib.nf_orthogonalize_work(dtype, count, rows, cols)
+    if n < 0:
+        raise NfError(NF_EINVAL, "nf_orthogonalize_work")
+    return n
+
+
+def nf_orthogonalize(x, out, work=None, stream=None) -> None:
+    """x: a matrix [rows][cols] or a stack [count][rows][cols] in fp32 or bf16; out of the
+    same type and shape, or x itself."""
+    code = _elem(x, "x")
+    if _elem(out, "out") != code or out.shape != x.shape:
+        raise ValueError("out must have x's type and shape")
+    p, count, rows, cols, ld, stride = _stack(x, "x")
+    o, _, _, _, ldo, so = _stack(out, "out")
+    w, n, keep = _workspace(work, _lib.nf_orthogonalize_work(code, count, rows, cols), stream, "nf_orthogonalize")
+    _check(_lib.nf_orthogonalize(p, code, count, rows, cols, ld, stride, o, ldo, so, w, n, _queue(stream)),
+           "nf_orthogonalize")
+
+
+def nf_muon_step(w, m, g, w_out, m_out, eta: float, momentum: float = 0.95, nesterov: bool = True,
+                 decay: float = 0.0, work=None, stream=None) -> None:
+    """One step on w ([rows][cols] or a stack) with gradient g and fp32 momentum m, into
+    w_out and m_out (which may be w and m).  All contiguous."""
+    import torch
+    wc, gc = _elem(w, "w"), _elem(g, "g")
+    shape = tuple(w.shape)
+    p, count, rows, cols, _, _ = _stack(w, "w")
+    f = torch.float32
+    wp = _vector(w, "w", w.dtype, shape)
+    gp = _vector(g, "g", g.dtype, shape)
+    k, n, keep = _workspace(work, _lib.nf_orthogonalize_work(wc, count, rows, cols), stream, "nf_muon_step")
+    _check(_lib.nf_muon_step(wp, wc, _vector(m, "m", f, shape), gp, gc, count, rows, cols, eta, momentum,
+                             int(nesterov), decay, _vector(w_out, "w_out", w.dtype, shape),
+                             _vector(m_out, "m_out", f, shape), k, n, _queue(stream)), "nf_muon_step")
+
+
+def _act(act) -> int:
+    return NF_NO_ACT if act is None else ACT_CODES[act] if isinstance(act, str) else int(act)
+
+
+def _bytes_matrix(t, name: str, rows: Optional[int] = None):
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor on the GPU")
+    if t.dtype != torch.int8 or not t.is_cuda:
+        raise ValueError(f"{name} must be an int8 GPU tensor")
+    p, r, c, ld = _matrix(t, name)
+    if rows is not None and r != rows:
+        raise ValueError(f"{name} must have {rows} rows")
+    return p, r, c, ld
+
+
+def nf_quantize_rows(x, q, scale, stream=None) -> None:
+    """x [rows][cols] into int8 q [rows][cols up to a multiple of 16, or more] and fp32
+    scale [rows]."""
+    import torch
+    code = _elem(x, "x")
+    p, rows, cols, ld = _matrix(x, "x")
+    qp, _, wide, ldq = _bytes_matrix(q, "q", rows)
+    if wide < (cols + 15) // 16 * 16:
+        raise ValueError("q must have x's columns, up to a multiple of 16")
+    _check(_lib.nf_quantize_rows(p, code, rows, cols, ld, qp, ldq, _vector(scale, "scale", torch.float32, (rows,)),
+                                 _queue(stream)), "nf_quantize_rows")
+
+
+def nf_linear_i8(xq, x_scale, wq, w_scale, y, inputs: int, bias=None, act=None, stream=None) -> None:
+    """y [rows][outputs] = act(x_scale w_scale (xq wq^T) + bias) of rows and weights
+    as nf_quantize_rows leaves them (int8 [..][inputs up to a multiple of 16])."""
+    import torch
+    xp, rows, xw, ldx = _bytes_matrix(xq, "xq")
+    wp, outs, ww, ldw = _bytes_matrix(wq, "wq")
+    wide = (inputs + 15) // 16 * 16
+    if xw < wide or ww < wide:
+        raise ValueError("xq and wq must hold the inputs, up to a multiple of 16")
+    f = torch.float32
+    yc = _elem(y, "y")
+    yp, _, _, ldy = _matrix(y, "y", (rows, outs))
+    _check(_lib.nf_linear_i8(xp, ldx, _vector(x_scale, "x_scale", f, (rows,)), wp, ldw,
+                             _vector(w_scale, "w_scale", f, (outs,)), _vector(bias, "bias", f, (outs,)), _act(act),
+                             rows, inputs, outs, yp, yc, ldy, _queue(stream)), "nf_linear_i8")
+
+
+def nf_linear_i8_dynamic(x, wq, w_scale, y, bias=None, act=None, work=None, stream=None) -> None:
+    """nf_linear_i8 of the rows x [rows][inputs], which it quantises."""
+    import torch
+    code, yc = _elem(x, "x"), _elem(y, "y")
+    xp, rows, cols, ldx = _matrix(x, "x")
+    wp, outs, ww, ldw = _bytes_matrix(wq, "wq")
+    if ww < (cols + 15) // 16 * 16:
+        raise ValueError("wq must hold x's columns, up to a multiple of 16")
+    f = torch.float32
+    yp, _, _, ldy = _matrix(y, "y", (rows, outs))
+    k, n, keep = _workspace(work, _lib.nf_linear_i8_work(rows, cols), stream, "nf_linear_i8_dynamic")
+    _check(_lib.nf_linear_i8_dynamic(xp, code, ldx, wp, ldw, _vector(w_scale, "w_scale", f, (outs,)),
+                                     _vector(bias, "bias", f, (outs,)), _act(act), rows, cols, outs, yp, yc, ldy,
+                                     k, n, _queue(stream)), "nf_linear_i8_dynamic")
 
 
 def nf_last_error() -> str:
