@@ -384,11 +384,12 @@ nf_status nf_logprobs_grad(const void* d_logits, int32_t dtype, int64_t rows, in
  * its singular vectors.  A matrix of zeros gives zeros; one with a NaN or an
  * infinity gives NaN throughout.
  * dtype: NF_F32 (products with fp32's precision) or NF_BF16 (products of fp16
- * values, sums and X itself in fp32).  ld and stride: elements from row to row and from
- * matrix to matrix; d_out may be d_x.
+ * values, sums and X itself in fp32).  ld (at most NF_ORTH_MAX_LD) and stride: elements from
+ * row to row and from matrix to matrix; d_out may be d_x.
  * d_work: nf_orthogonalize_work(dtype, count, rows, cols) bytes (-1 for sizes
  * that the call would refuse) aligned to 256. */
 #define NF_ORTH_MAX 65536
+#define NF_ORTH_MAX_LD (1 << 20)
 #define NF_ORTH_STEPS 5
 int64_t nf_orthogonalize_work(int32_t dtype, int64_t count, int64_t rows, int64_t cols);
 nf_status nf_orthogonalize(const void* d_x, int32_t dtype, int64_t count, int64_t rows,

@@ -169,61 +169,259 @@ __device__ __forceinline__ void with_act(int act, F&& f) {
     default: f(std::integral_constant<int, -1>()); break;
   }
 }
-__device__ __forceinline__ void put_y(void* y, int type, int64_t at, float v) {
-  if (type == NF_F32) static_cast<float*>(y)[at] = v;
-  else if (type == NF_BF16) static_cast<bf16_t*>(y)[at] = from_float<bf16_t>(v);
-  else static_cast<f16_t*>(y)[at] = from_float<f16_t>(v);
+// Four neighbours of a row of y, `n` of them inside it.  No activation hides that
+// a row could not be quantised.
+template <class T, int ACT>
+__device__ __forceinline__ void put_y(T* y, int n, const float (&z)[4]) {
+  T v[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) v[c] = from_float<T>(activated<ACT>(z[c]));
+  if (n >= 4) {
+    __builtin_memcpy(y, v, sizeof v);
+  } else {
+#pragma unroll
+    for (int c = 0; c < 3; ++c)
+      if (c < n) y[c] = v[c];
+  }
 }
 
-template <int BM, int BN, int WM, int WN, int NS, int OCC>
-__global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64, OCC) linear_kernel(const LinearArgs a) {
-  typedef MmTile<MM_I8, BM, BN, WM, WN, NS> Tile;
+template <class T, int BM, int BN, int WM, int WN, int NS, int G, int OCC>
+__global__ void __launch_bounds__((BM / WM) * (BN / WN) * G * 64, OCC) linear_kernel(const LinearArgs a) {
+  typedef MmTile<MM_I8, BM, BN, WM, WN, NS, G> Tile;
   __shared__ __attribute__((aligned(1024))) char lds[Tile::LDS];
   int bx, by;
   if (!mm_place(a.total, a.mt, a.nt, bx, by)) return;
   const int m0 = __builtin_amdgcn_readfirstlane(bx * BM), n0 = __builtin_amdgcn_readfirstlane(by * BN);
   const MmRows X{reinterpret_cast<const char*>(a.xq), a.ldx, a.rows};
   const MmRows Wt{reinterpret_cast<const char*>(a.wq), a.ldw, a.outputs};
-  typename Tile::Acc acc[Tile::TM][Tile::TN];
-  Tile::run(X, Wt, a.bytes, m0, n0, lds, acc);
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = (wave % (BM / WM)) * WM, wn = (wave / (BM / WM)) * WN;
+  Tile tile;
+  tile.run(X, Wt, a.bytes, m0, n0, lds);
+  // the scales and biases of the wave's rows and columns, zeros past the last
+  const auto xs = __builtin_amdgcn_make_buffer_rsrc((void*)a.x_scale, (short)0, a.rows * 4, 0x00020000);
+  const auto ws = __builtin_amdgcn_make_buffer_rsrc((void*)a.w_scale, (short)0, a.outputs * 4, 0x00020000);
+  const auto bs = __builtin_amdgcn_make_buffer_rsrc((void*)a.bias, (short)0, a.bias ? a.outputs * 4 : 0, 0x00020000);
+  float w4[Tile::TN][4], b4[Tile::TN][4], x1[Tile::TM][Tile::ROUNDS];
+#pragma unroll
+  for (int t = 0; t < Tile::TN; ++t)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const unsigned off = (unsigned)(n0 + tile.wn + t * 32 + tile.col() + c) * 4u;
+      w4[t][c] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(ws, off, 0, 0));
+      b4[t][c] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(bs, off, 0, 0));
+    }
+#pragma unroll
+  for (int t = 0; t < Tile::TM; ++t)
+#pragma unroll
+    for (int r = 0; r < Tile::ROUNDS; ++r)
+      x1[t][r] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(
+                                               xs, (unsigned)(m0 + tile.wm + t * 32 + tile.row(r)) * 4u, 0, 0));
+  T* const y = static_cast<T*>(a.y);
   with_act(a.act, [&](auto act) {
 #pragma unroll
-    for (int tj = 0; tj < Tile::TN; ++tj) {
-      const int j = n0 + wn + tj * 32 + (lane & 31);
-      if (j >= a.outputs) continue;
-      const float ws = a.w_scale[j], b = a.bias ? a.bias[j] : 0.f;
+    for (int b = 0; b < Tile::BLOCKS; ++b) {
+      const int ti = b / Tile::TN, tj = b % Tile::TN;
+      const int j = n0 + tile.wn + tj * 32 + tile.col();
+      tile.spread(b);
 #pragma unroll
-      for (int ti = 0; ti < Tile::TM; ++ti)
+      for (int r = 0; r < Tile::ROUNDS; ++r) {
+        int s[4];
+        tile.template sums<int>(r, s);
+        const int i = m0 + tile.wm + ti * 32 + tile.row(r);
+        float z[4];
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int i = m0 + wm + ti * 32 + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3);
-          if (i >= a.rows) continue;
-          const float z = (float)acc[ti][tj][v] * a.x_scale[i] * ws + b;
-          put_y(a.y, a.y_type, (int64_t)i * a.ldy + j, activated<act.value>(z));
-        }
+        for (int c = 0; c < 4; ++c) z[c] = (float)s[c] * x1[ti][r] * w4[tj][c] + b4[tj][c];
+        if (i < a.rows && j < a.outputs) put_y<T, act.value>(y + (int64_t)i * a.ldy + j, a.outputs - j, z);
+      }
     }
   });
 }
 
-template <int BM, int WM, int WN, int NS, int OCC>
+template <class T, int BM, int WM, int WN, int NS, int G, int OCC>
 hipError_t launch_linear_tile(LinearArgs a, hipStream_t s) {
   a.mt = (a.rows + BM - 1) / BM;
   a.nt = (a.outputs + BM - 1) / BM;
   a.total = a.mt * a.nt;
-  return launch_k(linear_kernel<BM, BM, WM, WN, NS, OCC>, dim3(mm_grid(a.total)), dim3((BM / WM) * (BM / WN) * 64), 0, s, a);
+  return launch_k(linear_kernel<T, BM, BM, WM, WN, NS, G, OCC>, dim3(mm_grid(a.total)),
+                  dim3((BM / WM) * (BM / WN) * G * 64), 0, s, a);
 }
 
-hipError_t launch_linear(const LinearArgs& a, int units, hipStream_t s) {
+// ---- few rows: the weights' bytes ----------------------------------------------
+// A workgroup forms 16 outputs of up to 16 rows.  Its 8 waves take turns along k, 64
+// bytes at a time, with operands straight from memory (16 rows of weights across the
+// lanes, 16 bytes each): the weights are read once, and nothing waits in LDS but the
+// sums of the waves.
+//
+// X not void: at most FEW_WAVES rows of X are quantised here, by every workgroup for itself, while its first
+// weights are on their way.
+constexpr int FEW_WAVES = 8;
+constexpr int FEW_AHEAD = 8;           // loads of weights a lane has under way
+constexpr int FEW_Q = 65536;           // bytes of quantised rows in LDS
+
+template <class X>
+struct FewArgs {
+  LinearArgs a;
+  const X* x;                          // [rows][ldf]
+  int64_t ldf;
+  int inputs;
+};
+
+template <class X, class T>
+__global__ void __launch_bounds__(64 * FEW_WAVES) linear_few_kernel(const FewArgs<X> f) {
+  constexpr bool QUANT = !std::is_void_v<X>;
+  const LinearArgs& a = f.a;
+  __shared__ int part[FEW_WAVES][256];
+  __shared__ __attribute__((aligned(16))) char q[QUANT ? FEW_Q : 16];
+  __shared__ float scales[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n0 = blockIdx.x * 16;
+  const int piece = (lane >> 4) * 16;                  // of 64 bytes of k
+  const int rows = a.rows;
+  const char* const w = reinterpret_cast<const char*>(a.wq) + (int64_t)min(n0 + (lane & 15), a.outputs - 1) * a.ldw;
+  const mm_i32x4 zero = {0, 0, 0, 0};
+  const int steps = (a.bytes + 63) / 64;
+  auto weights = [&](int s) {
+    const int k = s * 64 + piece;
+    return k < a.bytes ? *reinterpret_cast<const mm_i32x4*>(w + k) : zero;
+  };
+  mm_i32x4 wq[FEW_AHEAD];
+#pragma unroll
+  for (int u = 0; u < FEW_AHEAD; ++u) wq[u] = weights(wave + u * FEW_WAVES);
+  const char* xr;
+  if constexpr (QUANT) {
+    // one, two, four or all eight waves quantise a row; in LDS rows lie a pitch of
+    // steps 64-byte pieces and 16 bytes apart
+    constexpr int E = Vec16<X>::N;
+    const int pitch = steps * 64 + 16;
+    const int share = rows <= 1 ? 8 : rows <= 2 ? 4 : rows <= 4 ? 2 : 1;
+    const int r = wave / share, stride = share * 64 * E, j0 = ((wave % share) * 64 + lane) * E;
+    const X* const x = f.x + (int64_t)min(r, rows - 1) * f.ldf;
+    auto load = [&](int j) {
+      if (j + E <= f.inputs) return load16(x + j);
+      Vec16<X> v;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        v.v[e] = from_float<X>(0.f);
+        if (j + e < f.inputs) v.v[e] = x[j + e];
+      }
+      return v;
+    };
+    constexpr int KEEP = 2;              // vectors that need not be read again
+    Vec16<X> keep[KEEP];
+#pragma unroll
+    for (int u = 0; u < KEEP; ++u) keep[u] = load(j0 + u * stride);
+    float most = 0.f;
+    int nan = 0;
+    auto look = [&](const Vec16<X>& v) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float y = to_float(v.v[e]);
+        most = fmaxf(most, fabsf(y));
+        nan |= y != y;
+      }
+    };
+#pragma unroll
+    for (int u = 0; u < KEEP; ++u) look(keep[u]);
+#pragma unroll 4
+    for (int j = j0 + KEEP * stride; j < f.inputs; j += stride) look(load(j));
+    most = wave_max(most);
+    nan = __any(nan);
+    if (lane == 0) {
+      part[wave][0] = __builtin_bit_cast(int, most);
+      part[wave][1] = nan;
+    }
+    __syncthreads();
+    for (int g = r * share; g < (r + 1) * share; ++g) {
+      most = fmaxf(most, __builtin_bit_cast(float, part[g][0]));
+      nan |= part[g][1];
+    }
+    const RowScale rs = row_scale(most, nan);
+    auto put = [&](int j, const Vec16<X>& v) {
+      unsigned o[E / 4];
+#pragma unroll
+      for (int c = 0; c < E / 4; ++c) {
+        o[c] = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[c] |= (unsigned)(quantised(rs, to_float(v.v[4 * c + e])) & 255) << (8 * e);
+      }
+      if (j < steps * 64) __builtin_memcpy(q + r * pitch + j, o, E);
+    };
+    if (r < rows) {
+      if (lane == 0 && wave % share == 0) scales[r] = rs.scale;
+#pragma unroll
+      for (int u = 0; u < KEEP; ++u) put(j0 + u * stride, keep[u]);
+#pragma unroll 4
+      for (int j = j0 + KEEP * stride; j < steps * 64; j += stride) put(j, load(j));
+    }
+    __syncthreads();
+    xr = q + min(lane & 15, rows - 1) * pitch;
+  } else {
+    xr = reinterpret_cast<const char*>(a.xq) + (int64_t)min(lane & 15, rows - 1) * a.ldx;
+  }
+  mm_i32x4 acc = zero;
+  for (int s0 = wave; s0 < steps; s0 += FEW_WAVES * FEW_AHEAD) {
+#pragma unroll
+    for (int u = 0; u < FEW_AHEAD; ++u) {
+      const int s = s0 + u * FEW_WAVES, k = s * 64 + piece;
+      const mm_i32x4 now = wq[u];
+      wq[u] = weights(s + FEW_WAVES * FEW_AHEAD);
+      const mm_i32x4 x = k < a.bytes ? *reinterpret_cast<const mm_i32x4*>(xr + k) : zero;
+      acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, now, acc, 0, 0, 0);
+    }
+  }
+  // register v of a lane: row 4 (lane / 16) + v of x, output lane % 16
+#pragma unroll
+  for (int v = 0; v < 4; ++v) part[wave][v * 64 + lane] = acc[v];
+  __syncthreads();
+  if (tid >= 256) return;
+  const int r = 4 * ((tid & 63) >> 4) + (tid >> 6), n = n0 + (tid & 15);
+  int sum = 0;
+#pragma unroll
+  for (int g = 0; g < FEW_WAVES; ++g) sum += part[g][tid];
+  if (r >= rows || n >= a.outputs) return;
+  const float z = (float)sum * (QUANT ? scales[r] : a.x_scale[r]) * a.w_scale[n] + (a.bias ? a.bias[n] : 0.f);
+  with_act(a.act, [&](auto act) {
+    static_cast<T*>(a.y)[(int64_t)r * a.ldy + n] = from_float<T>(activated<act.value>(z));
+  });
+}
+
+template <class X, class T>
+hipError_t launch_few(const FewArgs<X>& f, hipStream_t s) {
+  return launch_k(linear_few_kernel<X, T>, dim3((unsigned)((f.a.outputs + 15) / 16)), dim3(64 * FEW_WAVES), 0, s, f);
+}
+
+// 16 rows are one operand of the matrix instruction; beyond, tiles of 64 x 64 that
+// share operands through LDS are faster (4096 x 4096, us: 16 rows 8.1, tiles 9.7; 32 rows,
+// two operands, 10.8, tiles 9.8; 784 -> 1024, 16 rows: 3.8, 5.5).  Up to four rows are quantised in
+// place, which saves a launch (4096 x 4096: 1 row 8.3, 10.2 with the launch; 4 rows 10.2, 11.1; 8 rows
+// 14.0, 11.6).
+bool few_rows(int64_t rows) { return rows <= 16; }
+bool few_quantises(int64_t rows, int64_t inputs) {
+  return rows <= 4 && rows * ((inputs + 63) / 64 * 64 + 16) <= FEW_Q;
+}
+
+template <class T>
+hipError_t launch_linear_as(const LinearArgs& a, int units, hipStream_t s) {
   auto tiles = [&](int64_t b) { return ((a.rows + b - 1) / b) * ((a.outputs + b - 1) / b); };
-  if (tiles(256) >= units) return launch_linear_tile<256, 128, 64, 2, 2>(a, s);
-  if (tiles(128) >= units) return launch_linear_tile<128, 64, 64, 2, 2>(a, s);
-  return launch_linear_tile<64, 32, 32, 3, 2>(a, s);
+  switch (mm_shape(tiles, units, (a.bytes + MM_STAGE - 1) / MM_STAGE)) {
+    case MM_64_GROUPS: return launch_linear_tile<T, 64, 32, 32, 3, 2, 2>(a, s);
+    case MM_64: return launch_linear_tile<T, 64, 32, 32, 3, 1, 3>(a, s);
+    case MM_128: return launch_linear_tile<T, 128, 64, 32, 2, 1, 4>(a, s);
+    case MM_192: return launch_linear_tile<T, 192, 96, 96, 3, 1, 1>(a, s);
+    default: return launch_linear_tile<T, 256, 128, 64, 2, 1, 2>(a, s);
+  }
+}
+hipError_t launch_linear(const LinearArgs& a, int units, hipStream_t s) {
+  return with_type(a.y_type, [&](auto e) {
+    typedef decltype(e) T;
+    if (few_rows(a.rows)) return launch_few<void, T>(FewArgs<void>{a, nullptr, 0, 0}, s);
+    return launch_linear_as<T>(a, units, s);
+  });
 }
 
 int64_t whole16(int64_t v) { return (v + 15) / 16 * 16; }
+// pitch of rows in the workspace: not a multiple of 4096, at which a tile's rows would
+// all lie in the same one of a cache's channels
+int64_t row_pitch(int64_t inputs) { return ((inputs + 127) / 128 | 1) * 128; }
 
 nf_status check_linear(const void* wq, int64_t ldw, const float* w_scale, int act, int64_t rows, int64_t inputs,
                        int64_t outputs, const void* y, int y_type, int64_t ldy) {
@@ -300,7 +498,7 @@ int64_t nf_linear_i8_work(int64_t rows, int64_t inputs) {
     op_fail(NF_ESHAPE, "at most %d inputs and 2^24 rows", NF_LINEAR_I8_MAX);
     return -1;
   }
-  return rows * whole16(inputs) + rows * 4;
+  return rows * row_pitch(inputs) + rows * 4;
 }
 
 nf_status nf_linear_i8_dynamic(const void* d_x, int32_t x_dtype, int64_t ld_x, const int8_t* d_wq, int64_t ld_w,
@@ -325,7 +523,17 @@ nf_status nf_linear_i8_dynamic(const void* d_x, int32_t x_dtype, int64_t ld_x, c
   const int units = op_compute_units();
   if (units <= 0) return op_fail(NF_EDEVICE, "no usable HIP device");
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const int64_t ldq = whole16(inputs);
+  if (few_quantises(rows, inputs))
+    return with_type(x_dtype, [&](auto xe) {
+      typedef decltype(xe) X;
+      return with_type(y_dtype, [&](auto ye) {
+        const LinearArgs a{nullptr, d_wq, 0, ld_w, ld_y, nullptr, d_w_scale, d_bias, act, (int)rows, (int)outputs,
+                           (int)whole16(inputs), y_dtype, d_y, 0, 0, 0};
+        const FewArgs<X> f{a, static_cast<const X*>(d_x), ld_x, (int)inputs};
+        return op_result(launch_few<X, decltype(ye)>(f, s), "8-bit linear layer");
+      });
+    });
+  const int64_t ldq = row_pitch(inputs);
   int8_t* const q = static_cast<int8_t*>(d_work);
   float* const scale = reinterpret_cast<float*>(q + rows * ldq);
   st = with_type(x_dtype, [&](auto e) {
@@ -334,7 +542,7 @@ nf_status nf_linear_i8_dynamic(const void* d_x, int32_t x_dtype, int64_t ld_x, c
   });
   if (st != NF_OK) return st;
   const LinearArgs a{q, d_wq, ldq, ld_w, ld_y, scale, d_w_scale, d_bias, act, (int)rows, (int)outputs,
-                     (int)ldq, y_dtype, d_y, 0, 0, 0};
+                     (int)whole16(inputs), y_dtype, d_y, 0, 0, 0};
   return op_result(launch_linear(a, units, s), "8-bit linear layer");
 }
 

@@ -6,18 +6,19 @@
 //   d(g log p_t + h H)/dx_j = scale (g ([j = t] - p_j) - h p_j (log p_j + H)).
 //
 // What bounds it: the bytes of the logits.  A row is read once into registers
-// where they hold it (up to 256 KB), so that the maximum, the sums, the
+// where they hold it (up to 128 KB), so that the maximum, the sums, the
 // alternatives and the gradient all come from one read; a longer row is read
 // with a running maximum and sum, and again for each of the others.  Rows of at
 // most 128 classes take 8 to 64 lanes of a wave.
 //
 // Alternatives: ordered(z) is a whole number in z's order, so (ordered(z),
 // ~index) orders by value and then by the lower index, and no two are equal.
-// Each wave finds the n_top-th largest of its lanes' maxima (32 ballots); the
-// largest of these is at most the row's n_top-th largest value, so the values
-// from there on hold all alternatives: they go to LDS (a few tens on logits of
-// some spread) and each counts the larger ones.  More than fit there (rows of
-// equal values) are found by n_top searches for the next largest instead.
+// The row's values fall into 64 groups, by the lanes that hold them; the n_top-th largest
+// of the groups' maxima (32 ballots of one wave) is at most the row's n_top-th largest
+// value, so the values from there on hold all alternatives (not many more, on
+// logits of some spread): the lanes whose own maximum is that large put them into LDS,
+// and each counts the larger ones.  More than fit there (rows of equal values)
+// are found by n_top searches for the next largest instead.
 #include "ops_common.h"
 
 namespace nf {
@@ -62,8 +63,16 @@ __device__ __forceinline__ float z_of(T x, float scale) {
   return to_float(x) * scale;
 }
 
-__device__ __forceinline__ float exp_of(float d) {
-  return __builtin_amdgcn_exp2f(d * 1.44269504088896340736f);
+constexpr float LOG2E = 1.44269504088896340736f;
+constexpr float LEAST = -1e5f;     // exp of it is 0, and 0 times it is 0
+
+__device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * LOG2E); }
+
+// exp(d) and its share of sum exp(d) d; a NaN comes through the exponential
+__device__ __forceinline__ void add_exp(float d, float& s, float& q) {
+  const float w = exp_of(d);
+  s += w;
+  q = fmaf(w, fmaxf(d, LEAST), q);
 }
 
 // What a row's sums come to.  A row whose classes are all at minus infinity has
@@ -85,14 +94,31 @@ __device__ __forceinline__ float log_prob(const RowSums& r, float z) {
   return r.empty ? -__builtin_inff() : (z - r.m) - r.ln;
 }
 
-// one value's place in the gradient, without the target's own share
+// A value's place in the gradient, without the target's own share:
+// -scale p (g + h (log p + H)), p = exp(z - m - log s).
 struct Slope {
-  float m, ln, g, h, entropy, scale;
-  bool empty;
+  float m, k, own;               // k = -log2 s; own: the target's share
+  float g, h, add;               // -scale g, -scale h, H - log s
+  bool entropies;
+  // a row that `has` a target of log probability, and its sums
+  __device__ __forceinline__ void set(float row_m, float ln, float entropy, float gi, float hi, float scale, bool none) {
+    // (of a row without probabilities every p is exp(-infinity))
+    m = none ? 0.f : row_m;
+    k = none ? -__builtin_inff() : -ln * LOG2E;
+    own = none ? 0.f : scale * gi;
+    g = -scale * gi;
+    h = -scale * hi;
+    add = none ? 0.f : entropy - ln;
+    entropies = hi != 0.f;         // NaN too
+  }
+  // EH: with the entropies' share
+  template <bool EH>
   __device__ __forceinline__ float at(float z) const {
-    const float d = z - m, p = exp_of(d - ln);
-    const float lp = p == 0.f ? 0.f : d - ln;       // 0 times the logarithm of 0 is 0
-    return empty ? 0.f : -scale * p * (g + h * (lp + entropy));
+    const float d = z - m;
+    const float p = __builtin_amdgcn_exp2f(fmaf(d, LOG2E, k));
+    if constexpr (!EH) return g * p;
+    // (0 times the logarithm of 0 is 0: d is bounded, a NaN comes through p)
+    return p * fmaf(h, fmaxf(d, LEAST) + add, g);
   }
 };
 
@@ -110,16 +136,42 @@ __device__ __forceinline__ void put_row(const LogpArgs<T>& a, int64_t row, const
 template <class T>
 __device__ __forceinline__ Slope slope_of(const LogpArgs<T>& a, int64_t row, const RowSums& r, int64_t t) {
   Slope s;
-  s.m = r.m;
-  s.ln = r.ln;
   // a row without a target has no log probability to change; a target past the
   // classes leaves no gradient that could be taken for one
-  s.g = t < 0 || !a.g ? 0.f : t >= a.classes ? __builtin_nanf("") : a.g[row];
-  s.h = a.h ? a.h[row] : 0.f;
-  s.entropy = r.entropy;
-  s.scale = a.scale;
-  s.empty = r.empty && t < a.classes;
+  const float g = t < 0 || !a.g ? 0.f : t >= a.classes ? __builtin_nanf("") : a.g[row];
+  s.set(r.m, r.ln, r.entropy, g, a.h ? a.h[row] : 0.f, a.scale, r.empty && t < a.classes);
   return s;
+}
+
+// A row's gradient: f(EH) with whether it has an entropies' share.
+template <class F>
+__device__ __forceinline__ void with_share(const Slope& sl, F&& f) {
+  if (sl.entropies) f(std::true_type());
+  else f(std::false_type());
+}
+
+// One vector's gradient; x0: its first class.
+template <bool EH, class T>
+__device__ __forceinline__ void put_slope(const Slope& sl, const Vec16<T>& v, float scale, T* dx, int j, int V, int64_t t) {
+  constexpr int E = Vec16<T>::N;
+  Vec16<T> o;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const float y = sl.at<EH>(z_of(v.v[e], scale));
+    o.v[e] = from_float<T>(y);
+  }
+  if (t >= j && t < j + E) {             // the vector that holds the target
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (j + e == t) o.v[e] = from_float<T>(sl.at<EH>(z_of(v.v[e], scale)) + sl.own);
+  }
+  if (j + E <= V) {
+    store16(dx + j, o);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (j + e < V) dx[j + e] = o.v[e];
+  }
 }
 
 // ---- rows of at most SMALL_MAX classes: G lanes a row, two values a lane -----
@@ -146,9 +198,7 @@ __global__ void __launch_bounds__(256) logp_small_kernel(const LogpArgs<T> a) {
   float s = 0.f, q = 0.f;
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
-    const float d = z[e] - mm, w = exp_of(d);
-    s += w;
-    q += w == 0.f ? 0.f : w * d;
+    add_exp(z[e] - mm, s, q);
   }
 #pragma unroll
   for (int o = G / 2; o >= 1; o >>= 1) {
@@ -186,8 +236,8 @@ __global__ void __launch_bounds__(256) logp_small_kernel(const LogpArgs<T> a) {
     for (int e = 0; e < 2; ++e)
       if (live && in[e]) {
         const int j = at + e * G;
-        const float own = j == t && !sl.empty ? sl.scale * sl.g : 0.f;
-        a.dx[row * a.ld_dx + j] = from_float<T>(sl.at(z[e]) + own);
+        const float y = sl.entropies ? sl.at<true>(z[e]) : sl.at<false>(z[e]);
+        a.dx[row * a.ld_dx + j] = from_float<T>(y + (j == t ? sl.own : 0.f));
       }
   }
 }
@@ -196,8 +246,8 @@ __global__ void __launch_bounds__(256) logp_small_kernel(const LogpArgs<T> a) {
 template <int W>
 struct BlockShare {
   float m[W], s[W], q[W];
-  unsigned top[W];
-  float zt;
+  unsigned lane[64 * W];
+  unsigned from;
   int count;
   unsigned long long best[W];
   unsigned long long key[TOP_CAP];
@@ -229,6 +279,17 @@ __global__ void __launch_bounds__(THREADS) logp_row_kernel(const LogpArgs<T> a) 
 #pragma unroll
     for (int v = 0; v < NV; ++v) keep[v] = load((v * THREADS + tid) * E);
   }
+  // The row's values are wanted anew: what was made of them is not kept in registers.
+  auto again = [&] {
+    if constexpr (NV > 0) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        uint4 u = __builtin_bit_cast(uint4, keep[v]);
+        asm volatile("" : "+v"(u.x), "+v"(u.y), "+v"(u.z), "+v"(u.w));
+        keep[v] = __builtin_bit_cast(Vec16<T>, u);
+      }
+    }
+  };
   // f(j, vector): each of the thread's vectors that begins inside the row
   auto each = [&](auto&& f) {
     if constexpr (NV > 0) {
@@ -255,20 +316,18 @@ __global__ void __launch_bounds__(THREADS) logp_row_kernel(const LogpArgs<T> a) 
   if (tid == 0 && t >= 0 && t < V) zt = z_of(x[t], a.scale);
 
   // maximum and sums
-  float m = -__builtin_inff(), s = 0.f, q = 0.f;
+  float m = -__builtin_inff(), s = 0.f, q = 0.f, lane_max;
   auto add = [&](const Vec16<T>& r, float mm) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const float d = z_of(r.v[e], a.scale) - mm, w = exp_of(d);
-      s += w;
-      q += w == 0.f ? 0.f : w * d;
-    }
+    for (int e = 0; e < E; ++e) add_exp(z_of(r.v[e], a.scale) - mm, s, q);
   };
   if constexpr (NV > 0) {
+    // (scale > 0 keeps the order, also as rounded)
     each([&](int, const Vec16<T>& r) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) m = fmaxf(m, z_of(r.v[e], a.scale));
+      for (int e = 0; e < E; ++e) m = fmaxf(m, to_float(r.v[e]));
     });
+    lane_max = m = z_of(m, a.scale);
     m = wave_max(m);
     if constexpr (W > 1) {
       if (lane == 0) sh.m[wave] = m;
@@ -278,6 +337,7 @@ __global__ void __launch_bounds__(THREADS) logp_row_kernel(const LogpArgs<T> a) 
       for (int w = 1; w < W; ++w) m = fmaxf(m, sh.m[w]);
     }
     m = m == -__builtin_inff() ? 0.f : m;
+    again();
     each([&](int, const Vec16<T>& r) { add(r, m); });
   } else {
     // running: the sums are relative to the thread's maximum so far
@@ -296,6 +356,7 @@ __global__ void __launch_bounds__(THREADS) logp_row_kernel(const LogpArgs<T> a) 
       add(r, m);
     });
     const float own = run;
+    lane_max = run;
     m = wave_max(run);
     if (lane == 0) sh.m[wave] = m;
     __syncthreads();
@@ -334,54 +395,51 @@ __global__ void __launch_bounds__(THREADS) logp_row_kernel(const LogpArgs<T> a) 
   if constexpr (GRAD) {
     const Slope sl = slope_of(a, row, r, t);
     T* const dx = a.dx + row * a.ld_dx;
-    const float own = sl.empty ? 0.f : sl.scale * sl.g;
-    each([&](int j, const Vec16<T>& v) {
-      Vec16<T> o;
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        o.v[e] = from_float<T>(sl.at(z_of(v.v[e], a.scale)) + (j + e == t ? own : 0.f));
-      if (j + E <= V) {
-        store16(dx + j, o);
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (j + e < V) dx[j + e] = o.v[e];
-      }
+    again();
+    with_share(sl, [&](auto eh) {
+      each([&](int j, const Vec16<T>& v) { put_slope<eh.value>(sl, v, a.scale, dx, j, V, t); });
     });
     return;
   }
   if (a.n_top <= 0) return;
 
-  // the largest of the waves' n_top-th largest lane maxima
-  unsigned most = 0;
-  each([&](int j, const Vec16<T>& v) {
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-      if (j + e < V) most = max(most, ordered(z_of(v.v[e], a.scale)));
-  });
-  unsigned from = 0;
-#pragma unroll
-  for (int b = 31; b >= 0; --b) {
-    const unsigned c = from | (1u << b);
-    if (__popcll(__ballot(most >= c)) >= a.n_top) from = c;
-  }
+  // The n_top-th largest of 64 maxima, each of the lanes of one place in all waves.
+  // (A lane that met nothing but NaN has minus infinity: no more than the values there.)
+  unsigned from = ordered(lane_max);
   if constexpr (W > 1) {
-    if (lane == 0) sh.top[wave] = from;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < W; ++w) from = max(from, sh.top[w]);
-  } else {
+    sh.lane[tid] = from;
     __syncthreads();
   }
-  from = max(from, 1u);
-  if (most >= from)
+  if (wave == 0) {
+    unsigned most = from;
+#pragma unroll
+    for (int w = 1; w < W; ++w) most = max(most, sh.lane[w * 64 + lane]);
+    from = 0;
+#pragma unroll
+    for (int b = 31; b >= 0; --b) {
+      const unsigned c = from | (1u << b);
+      if (__popcll(__ballot(most >= c)) >= a.n_top) from = c;
+    }
+    if constexpr (W > 1)
+      if (lane == 0) sh.from = from;
+  }
+  __syncthreads();
+  if constexpr (W > 1) from = sh.from;
+  const float least = unordered(from);
+  again();
+  const bool bad = s != s;                       // a NaN in the row: no maximum tells where
+  if (lane_max >= least || bad)
     each([&](int j, const Vec16<T>& v) {
+      float top = to_float(v.v[0]);
+#pragma unroll
+      for (int e = 1; e < E; ++e) top = fmaxf(top, to_float(v.v[e]));
+      if (z_of(top, a.scale) < least && !bad) return;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const unsigned k = j + e < V ? ordered(z_of(v.v[e], a.scale)) : 0u;
-        if (k >= from) {
+        const float z = z_of(v.v[e], a.scale);
+        if (!(z < least) && j + e < V) {         // a NaN too
           const int at = atomicAdd(&sh.count, 1);
-          if (at < TOP_CAP) sh.key[at] = (unsigned long long)k << 32 | (unsigned)~(unsigned)(j + e);
+          if (at < TOP_CAP) sh.key[at] = (unsigned long long)ordered(z) << 32 | (unsigned)~(unsigned)(j + e);
         }
       }
     });
@@ -404,6 +462,7 @@ __global__ void __launch_bounds__(THREADS) logp_row_kernel(const LogpArgs<T> a) 
   unsigned long long last = ~0ull;      // above every key: the lowest index of a NaN has a smaller one
   for (int k = 0; k < a.n_top; ++k) {
     unsigned long long best = 0;
+    again();
     each([&](int j, const Vec16<T>& v) {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
@@ -469,34 +528,21 @@ __global__ void __launch_bounds__(256) logp_grad_kernel(const GradArgs<T> a) {
   }
   const int64_t t = a.target ? a.target[row] : -1;
   Slope sl;
-  sl.m = a.stat[2 * row];
-  sl.ln = a.stat[2 * row + 1];
-  sl.g = t < 0 || !a.g ? 0.f : t >= V ? __builtin_nanf("") : a.g[row];
-  sl.h = a.h ? a.h[row] : 0.f;
-  sl.entropy = a.h ? a.entropy[row] : 0.f;
-  sl.scale = a.scale;
-  sl.empty = sl.ln == -__builtin_inff() && t < V;
-  const float own = sl.empty ? 0.f : sl.scale * sl.g;
+  const float ln = a.stat[2 * row + 1];
+  sl.set(a.stat[2 * row], ln, a.h ? a.entropy[row] : 0.f, t < 0 || !a.g ? 0.f : t >= V ? __builtin_nanf("") : a.g[row],
+         a.h ? a.h[row] : 0.f, a.scale, ln == -__builtin_inff() && t < V);
+  with_share(sl, [&](auto eh) {
 #pragma unroll
-  for (int u = 0; u < GRAD_VECS; ++u) {
-    const int j = first + (u * 256 + (int)threadIdx.x) * E;
-    Vec16<T> o;
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-      o.v[e] = from_float<T>(sl.at(z_of(v[u].v[e], a.scale)) + (j + e == t ? own : 0.f));
-    if (j + E <= V) {
-      store16(dx + j, o);
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (j + e < V) dx[j + e] = o.v[e];
+    for (int u = 0; u < GRAD_VECS; ++u) {
+      const int j = first + (u * 256 + (int)threadIdx.x) * E;
+      if (j < V) put_slope<eh.value>(sl, v[u], a.scale, dx, j, V, t);
     }
-  }
+  });
 }
 
 // ---- launches ----------------------------------------------------------------
 template <class T, bool GRAD>
-hipError_t launch_logp(const LogpArgs<T>& a, hipStream_t s) {
+hipError_t launch_logp(const LogpArgs<T>& a, int units, hipStream_t s) {
   if (a.classes <= SMALL_MAX) {
     const int half = (a.classes + 1) / 2;
     auto go = [&](auto g) {
@@ -510,19 +556,36 @@ hipError_t launch_logp(const LogpArgs<T>& a, hipStream_t s) {
     return go(std::integral_constant<int, 64>());
   }
   const int64_t vecs = (a.classes + Vec16<T>::N - 1) / Vec16<T>::N;
+  // Threads of a workgroup and vectors in a thread's registers, as measured (us, MI355X):
+  //   no gradient, 256 threads and 2 vectors, against none in registers: 8192 x 2500 bf16 with 8
+  //   alternatives 27, 33.  Longer rows are read in passes, the second (for alternatives) by few
+  //   lanes: 8192 x 16000 bf16 by 256 threads 101, 512 137, 512 and 4 vectors 126;
+  //   2049 x 50021 bf16 by 256 80, by 512 75; 1000 x 131072 f32 by 256 119, 512 107, 1024 102.
+  //   Gradient: 8192 x 5000 bf16, 256 and 4 46, 256 and none 58; 4096 x 32768 bf16, 512 and 8 120,
+  //   1024 and 4 124, 512 and none 147; 4096 x 16384 f32 113, 108, 123; 600 x 50000 bf16, 512 and none 41,
+  //   1024 54, 1024 and 8 51; 1000 x 131072 bf16 by 512 177, by 1024 170.
+  //   Few rows wait for one another's steps, so more threads: 1 x 32768 bf16, 1024 and 4 7.5, 512 and 8
+  //   8.2; 20 x 50000 f32 by 1024 15, by 512 17.
 #define NF_ROW(TH, NV) \
-  if (vecs <= (int64_t)(TH) * (NV))  \
-    return launch_k(logp_row_kernel<T, TH, NV, GRAD>, dim3((unsigned)a.rows), dim3(TH), 0, s, a);
-  NF_ROW(64, 1)
-  NF_ROW(64, 4)
-  NF_ROW(256, 2)
-  NF_ROW(256, 4)
-  NF_ROW(256, 8)
-  NF_ROW(1024, 4)
-  NF_ROW(1024, 8)
-  NF_ROW(1024, 16)
+  return launch_k(logp_row_kernel<T, TH, NV, GRAD>, dim3((unsigned)a.rows), dim3(TH), 0, s, a)
+  const bool few = a.rows <= units;
+  if (vecs <= 64) NF_ROW(64, 1);
+  if (vecs <= 256) NF_ROW(64, 4);
+  if (vecs <= 512) NF_ROW(256, 2);
+  if constexpr (GRAD) {
+    if (vecs <= 1024) NF_ROW(256, 4);
+    if (vecs <= 2048) NF_ROW(512, 4);
+    if (vecs <= 4096) {
+      if (sizeof(T) == 4 || few) NF_ROW(1024, 4);
+      NF_ROW(512, 8);
+    }
+  } else {
+    if (few && vecs <= 4096) NF_ROW(1024, 4);
+    if (!few && vecs <= 4096) NF_ROW(256, 0);
+  }
+  if (!few && vecs <= 16384) NF_ROW(512, 0);
+  NF_ROW(1024, 0);
 #undef NF_ROW
-  return launch_k(logp_row_kernel<T, 1024, 0, GRAD>, dim3((unsigned)a.rows), dim3(1024), 0, s, a);
 }
 
 nf_status check_logits(const void* x, int dtype, int64_t rows, int64_t classes, int64_t ld, float scale) {
@@ -590,7 +653,8 @@ nf_status nf_logprobs(const void* d_logits, int32_t dtype, int64_t rows, int64_t
   if (n_top > classes) return op_fail(NF_ESHAPE, "more alternatives than classes");
   if (n_top > 0 && !d_top_ids && !d_top_logp) return op_fail(NF_EINVAL, "alternatives without a place for them");
   if (rows == 0) return NF_OK;
-  if (op_compute_units() <= 0) return op_fail(NF_EDEVICE, "no usable HIP device");
+  const int units = op_compute_units();
+  if (units <= 0) return op_fail(NF_EDEVICE, "no usable HIP device");
   return with_type(dtype, [&](auto e) {
     typedef decltype(e) T;
     LogpArgs<T> a{};
@@ -606,7 +670,7 @@ nf_status nf_logprobs(const void* d_logits, int32_t dtype, int64_t rows, int64_t
     a.stat = d_stat;
     a.top_ids = d_top_ids;
     a.top_logp = d_top_logp;
-    return op_result(launch_logp<T, false>(a, static_cast<hipStream_t>(stream)), "log probabilities");
+    return op_result(launch_logp<T, false>(a, units, static_cast<hipStream_t>(stream)), "log probabilities");
   });
 }
 
@@ -621,7 +685,8 @@ nf_status nf_logprobs_train(const void* d_logits, int32_t dtype, int64_t rows, i
   if (d_g_logp && !d_targets) return op_fail(NF_EINVAL, "weights of log probabilities without targets");
   st = check_gradient(d_logits, ld, d_dlogits, ld_d, dtype, rows, classes);
   if (st != NF_OK) return st;
-  if (op_compute_units() <= 0) return op_fail(NF_EDEVICE, "no usable HIP device");
+  const int units = op_compute_units();
+  if (units <= 0) return op_fail(NF_EDEVICE, "no usable HIP device");
   return with_type(dtype, [&](auto e) {
     typedef decltype(e) T;
     LogpArgs<T> a{};
@@ -638,7 +703,7 @@ nf_status nf_logprobs_train(const void* d_logits, int32_t dtype, int64_t rows, i
     a.entropy = d_entropy;
     a.stat = d_stat;
     a.dx = static_cast<T*>(d_dlogits);
-    return op_result(launch_logp<T, true>(a, static_cast<hipStream_t>(stream)), "log probabilities and gradient");
+    return op_result(launch_logp<T, true>(a, units, static_cast<hipStream_t>(stream)), "log probabilities and gradient");
   });
 }
 
@@ -655,7 +720,8 @@ nf_status nf_logprobs_grad(const void* d_logits, int32_t dtype, int64_t rows, in
   if (d_g_entropy && !d_entropy) return op_fail(NF_EINVAL, "weights of entropies without the entropies");
   st = check_gradient(d_logits, ld, d_dlogits, ld_d, dtype, rows, classes);
   if (st != NF_OK) return st;
-  if (op_compute_units() <= 0) return op_fail(NF_EDEVICE, "no usable HIP device");
+  const int units = op_compute_units();
+  if (units <= 0) return op_fail(NF_EDEVICE, "no usable HIP device");
   return with_type(dtype, [&](auto e) {
     typedef decltype(e) T;
     GradArgs<T> a{};

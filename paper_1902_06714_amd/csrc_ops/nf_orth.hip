@@ -25,6 +25,7 @@
 // rows.
 #include <cmath>
 
+#include "orth_small.h"
 #include "rows_mm.h"
 
 namespace nf {
@@ -32,18 +33,12 @@ namespace {
 
 constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
 constexpr float UNIT = 16384.f, PER_UNIT = 1.f / UNIT;
-constexpr int SUM_BLOCKS = 256;        // at most; partial sums of a matrix
+constexpr int SUM_BLOCKS = 1024;       // at most; partial sums of a matrix
 
 // where element (r, c) of an operand lies; its second part 64 bytes on
 template <int KIND>
 __device__ __forceinline__ int64_t place(int64_t r, int c, int64_t pitch) {
   return KIND == MM_PARTS2 ? r * pitch + (c / PARTS2_GROUP) * 128 + (c % PARTS2_GROUP) * 2 : r * pitch + c * 2;
-}
-template <int KIND>
-__device__ __forceinline__ void put_value(char* p, int64_t at, float x) {
-  const _Float16 h = (_Float16)x;
-  *reinterpret_cast<_Float16*>(p + at) = h;
-  if constexpr (KIND == MM_PARTS2) *reinterpret_cast<_Float16*>(p + at + 64) = (_Float16)(x - (float)h);
 }
 template <int KIND>
 __device__ __forceinline__ void put_four(char* p, int64_t at, const float (&x)[4]) {
@@ -56,17 +51,12 @@ __device__ __forceinline__ void put_four(char* p, int64_t at, const float (&x)[4
   *reinterpret_cast<f16x4*>(p + at) = h;
   if constexpr (KIND == MM_PARTS2) *reinterpret_cast<f16x4*>(p + at + 64) = l;
 }
-template <int KIND>
-__device__ __forceinline__ float get_value(const char* p, int64_t at) {
-  float x = (float)*reinterpret_cast<const _Float16*>(p + at);
-  if constexpr (KIND == MM_PARTS2) x += (float)*reinterpret_cast<const _Float16*>(p + at + 64);
-  return x;
-}
 
 // The buffers of one matrix (offsets in its share of the workspace; pitches in
-// bytes, whole stages).
+// bytes).
 struct OrthPlan {
   int m, n;                   // shorter and longer side
+  int kx, kt;                 // bytes of a row of n, of m, whole stages, the last with zeros
   int64_t px, pt, pm;         // pitches of rows of n, of rows of m, of the fp32 X
   int64_t x, xt[2], a, b, xm, da, db, sums;
   int64_t bytes;              // of one matrix
@@ -74,13 +64,20 @@ struct OrthPlan {
 
 int64_t up(int64_t v, int64_t a) { return (v + a - 1) / a * a; }
 
+// A pitch of at least `bytes` that is an odd number of stages: rows whose pitch is
+// a multiple of 4096 bytes begin in the same one of a cache's channels, and a tile's
+// rows would all be read from it at one time.
+int64_t odd_pitch(int64_t bytes) { return (up(bytes, 128) / 128 | 1) * 128; }
+
 OrthPlan orth_plan(bool parts, int64_t rows, int64_t cols) {
   OrthPlan p{};
   p.m = (int)(rows < cols ? rows : cols);
   p.n = (int)(rows < cols ? cols : rows);
-  p.px = parts ? up(p.n, 32) * 4 : up(p.n, 64) * 2;
-  p.pt = parts ? up(p.m, 32) * 4 : up(p.m, 64) * 2;
-  p.pm = parts ? 0 : up(p.n, 64) * 4;
+  p.kx = (int)up((int64_t)p.n * (parts ? 4 : 2), 128);
+  p.kt = (int)up((int64_t)p.m * (parts ? 4 : 2), 128);
+  p.px = odd_pitch(p.kx);
+  p.pt = odd_pitch(p.kt);
+  p.pm = parts ? 0 : odd_pitch(2 * (int64_t)p.kx);
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
     const int64_t r = at;
@@ -100,13 +97,6 @@ OrthPlan orth_plan(bool parts, int64_t rows, int64_t cols) {
   return p;
 }
 
-// A stack of matrices in memory, in elements.
-template <class T>
-struct Stack {
-  T* p;
-  int64_t ld, stride;
-};
-
 // ---- U, its momentum and the sum of its squares ------------------------------
 template <class T>
 struct SumArgs {
@@ -119,10 +109,6 @@ struct SumArgs {
   char* work;
   int64_t share, sums;        // bytes of a matrix's share, offset of its sums
 };
-
-__device__ __forceinline__ float direction(float g, float m, float momentum, bool nesterov) {
-  return nesterov ? fmaf(momentum, m, g) : m;
-}
 
 template <class T>
 __global__ void __launch_bounds__(256) orth_sum_kernel(const SumArgs<T> a) {
@@ -195,7 +181,8 @@ __global__ void __launch_bounds__(256) orth_fill_kernel(const FillArgs<T> a) {
   __shared__ float tile[64][65];
   __shared__ double part[4];
   const int tid = threadIdx.x;
-  double s = tid < a.blocks ? reinterpret_cast<const double*>(w + p.sums)[tid] : 0.0;
+  double s = 0.0;
+  for (int i = tid; i < a.blocks; i += 256) s += reinterpret_cast<const double*>(w + p.sums)[i];
   s = wave_sum(s);
   if ((tid & 63) == 0) part[tid >> 6] = s;
   __syncthreads();
@@ -205,23 +192,32 @@ __global__ void __launch_bounds__(256) orth_fill_kernel(const FillArgs<T> a) {
   const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;
   const T* const g = a.g.p + (int64_t)blockIdx.z * a.g.stride;
   const float* const mom = a.m.p ? a.m.p + (int64_t)blockIdx.z * a.m.stride : nullptr;
-  for (int e = tid; e < 64 * 64; e += 256) {
-    // lanes along the user's rows
-    const int c = e & 63, r = e >> 6;
-    const int i = i0 + (a.turned ? c : r), j = j0 + (a.turned ? r : c);
-    float v = 0.f;
-    if (i < p.m && j < p.n) {
-      const int64_t ur = a.turned ? j : i, uc = a.turned ? i : j;
-      float u = to_float(g[ur * a.g.ld + uc]);
-      if (mom) u = direction(u, mom[ur * a.m.ld + uc], a.momentum, a.nesterov);
-      v = (float)((double)u * inv);
-      if (inv != inv) v = __builtin_nanf("");
+#pragma unroll
+  for (int e0 = 0; e0 < 64 * 64; e0 += 8 * 256) {
+    // lanes along the user's rows; the loads of 8 values are under way together
+    // (places past the matrix read its first value instead)
+    float u[8], m[8];
+    bool in[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int e = e0 + k * 256 + tid, c = e & 63, r = e >> 6;
+      const int i = i0 + (a.turned ? c : r), j = j0 + (a.turned ? r : c);
+      in[k] = i < p.m && j < p.n;
+      const int64_t ur = in[k] ? a.turned ? j : i : 0, uc = in[k] ? a.turned ? i : j : 0;
+      u[k] = to_float(g[ur * a.g.ld + uc]);
+      if (mom) m[k] = mom[ur * a.m.ld + uc];
     }
-    if (a.turned) tile[c][r] = v;
-    else tile[r][c] = v;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int e = e0 + k * 256 + tid, c = e & 63, r = e >> 6;
+      if (mom) u[k] = direction(u[k], m[k], a.momentum, a.nesterov);
+      const float v = !in[k] ? 0.f : inv != inv ? __builtin_nanf("") : (float)((double)u[k] * inv);
+      if (a.turned) tile[c][r] = v;
+      else tile[r][c] = v;
+    }
   }
   __syncthreads();
-  const int nx = (int)(p.px / (KIND == MM_PARTS2 ? 4 : 2)), nt = (int)(p.pt / (KIND == MM_PARTS2 ? 4 : 2));
+  const int nx = p.kx / (KIND == MM_PARTS2 ? 4 : 2), nt = p.kt / (KIND == MM_PARTS2 ? 4 : 2);
   for (int e = tid; e < 64 * 16; e += 256) {
     const int r = e >> 4, c = (e & 15) * 4;
     if (i0 + r < p.m && j0 + c < nx) {
@@ -255,29 +251,97 @@ struct MmArgs {
   float keep, rate;           // w' = keep w - rate X
 };
 
-__device__ __forceinline__ void put_result(const MmArgs& a, int z, int64_t r, int64_t c, float x) {
-  const int64_t o = z * a.stride_o + r * a.ldo + c;
-  if (a.w) {
-    const int64_t i = z * a.stride_w + r * a.ldw + c;
-    const float w = a.out_type == NF_F32 ? static_cast<const float*>(a.w)[i]
-                                         : to_float(static_cast<const bf16_t*>(a.w)[i]);
-    x = fmaf(-a.rate, x, a.keep * w);
+typedef unsigned mm_u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned mm_u32x4 __attribute__((ext_vector_type(4)));
+typedef float mm_f32x4 __attribute__((ext_vector_type(4)));
+
+// The rows of a matrix from row r0 on as a buffer: what lies at TILE_OOB reads as
+// zero and is not stored, so that an epilogue needs no branches and its loads do
+// not wait for one another.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(void* p, int64_t r0, int64_t pitch) {
+  return __builtin_amdgcn_make_buffer_rsrc(static_cast<char*>(p) + r0 * pitch, (short)0, (int)TILE_OOB, 0x00020000);
+}
+__device__ __forceinline__ float load_f32(const __amdgpu_buffer_rsrc_t& r, unsigned off) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0));
+}
+__device__ __forceinline__ void store_f32(const __amdgpu_buffer_rsrc_t& r, unsigned off, float x) {
+  __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, x), r, off, 0, 0);
+}
+template <int KIND>
+__device__ __forceinline__ unsigned across(int c) {       // bytes from a row's beginning to its element c
+  return KIND == MM_PARTS2 ? (unsigned)((c / PARTS2_GROUP) * 128 + (c % PARTS2_GROUP) * 2) : (unsigned)(c * 2);
+}
+template <int KIND>
+struct Four {                                             // four elements of a row, as they are loaded
+  f16x4 h, l;
+  __device__ __forceinline__ void load(const __amdgpu_buffer_rsrc_t& r, unsigned off) {
+    h = __builtin_bit_cast(f16x4, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0));
+    if constexpr (KIND == MM_PARTS2) l = __builtin_bit_cast(f16x4, __builtin_amdgcn_raw_buffer_load_b64(r, off + 64u, 0, 0));
   }
-  if (a.out_type == NF_F32)
-    static_cast<float*>(a.out)[o] = x;
-  else
-    static_cast<bf16_t*>(a.out)[o] = from_float<bf16_t>(x);
+  __device__ __forceinline__ float operator[](int c) const {
+    return KIND == MM_PARTS2 ? (float)h[c] + (float)l[c] : (float)h[c];
+  }
+};
+template <int KIND>
+__device__ __forceinline__ void store_four(const __amdgpu_buffer_rsrc_t& r, unsigned off, const float (&x)[4]) {
+  f16x4 h, l;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    h[c] = (_Float16)x[c];
+    l[c] = (_Float16)(x[c] - (float)h[c]);
+  }
+  __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(mm_u32x2, h), r, off, 0, 0);
+  if constexpr (KIND == MM_PARTS2) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(mm_u32x2, l), r, off + 64u, 0, 0);
 }
 
-template <int KIND, int PROD, int BM, int BN, int WM, int WN, int NS, int OCC>
-__global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64, OCC) orth_mm_kernel(const MmArgs a) {
-  typedef MmTile<KIND, BM, BN, WM, WN, NS> Tile;
+// four neighbours of a row of the user's matrix; `n` of them are inside it
+__device__ __forceinline__ void load_user(const void* p, int type, int64_t at, int n, float (&x)[4]) {
+  auto go = [&](auto e) {
+    typedef decltype(e) T;
+    const T* const q = static_cast<const T*>(p) + at;
+    T v[4] = {};
+    if (n >= 4) {
+      __builtin_memcpy(v, q, sizeof v);
+    } else {
+#pragma unroll
+      for (int c = 0; c < 3; ++c)
+        if (c < n) v[c] = q[c];
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) x[c] = to_float(v[c]);
+  };
+  if (type == NF_F32) go(float());
+  else go(bf16_t());
+}
+__device__ __forceinline__ void store_user(void* p, int type, int64_t at, int n, const float (&x)[4]) {
+  auto go = [&](auto e) {
+    typedef decltype(e) T;
+    T* const q = static_cast<T*>(p) + at;
+    T v[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) v[c] = from_float<T>(x[c]);
+    if (n >= 4) {
+      __builtin_memcpy(q, v, sizeof v);
+    } else {
+#pragma unroll
+      for (int c = 0; c < 3; ++c)
+        if (c < n) q[c] = v[c];
+    }
+  };
+  if (type == NF_F32) go(float());
+  else go(bf16_t());
+}
+
+template <int KIND, int PROD, int BM, int BN, int WM, int WN, int NS, int G, int OCC>
+__global__ void __launch_bounds__((BM / WM) * (BN / WN) * G * 64, OCC) orth_mm_kernel(const MmArgs a) {
+  typedef MmTile<KIND, BM, BN, WM, WN, NS, G> Tile;
   __shared__ __attribute__((aligned(1024))) char lds[Tile::LDS];
+  constexpr bool SQUARE = PROD == PROD_GRAM || PROD == PROD_POLY;
   const OrthPlan& p = a.p;
   const int z = blockIdx.y;
   char* const w = a.work + z * p.bytes;
   int bx, by;
-  if constexpr (PROD == PROD_GRAM || PROD == PROD_POLY) {
+  if constexpr (SQUARE) {
     static_assert(BM == BN, "square tiles");
     if (!mm_place_lower(a.total, bx, by)) return;
   } else {
@@ -285,124 +349,171 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64, OCC) orth_mm_kerne
   }
   const int m0 = __builtin_amdgcn_readfirstlane(bx * BM), n0 = __builtin_amdgcn_readfirstlane(by * BN);
   const MmRows X{w + p.x, p.px, p.m}, XT{w + p.xt[a.from], p.pt, p.n}, A{w + p.a, p.pt, p.m}, B{w + p.b, p.pt, p.m};
-  typename Tile::Acc acc[Tile::TM][Tile::TN];
+  const bool turned = PROD == PROD_LAST && a.turned;     // rows of X^T down, rows of B across
+  Tile tile;
   if constexpr (PROD == PROD_GRAM)
-    Tile::run(X, X, (int)p.px, m0, n0, lds, acc);
+    tile.run(X, X, p.kx, m0, n0, lds);
   else if constexpr (PROD == PROD_POLY)
-    Tile::run(A, A, (int)p.pt, m0, n0, lds, acc);
-  else if (PROD == PROD_LAST && a.turned)
-    Tile::run(XT, B, (int)p.pt, m0, n0, lds, acc);
+    tile.run(A, A, p.kt, m0, n0, lds);
   else
-    Tile::run(B, XT, (int)p.pt, m0, n0, lds, acc);
+    tile.run(turned ? XT : B, turned ? B : XT, p.kt, m0, n0, lds);
 
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = (wave % (BM / WM)) * WM, wn = (wave / (BM / WM)) * WN;
-  const int per = KIND == MM_PARTS2 ? 4 : 2;
-  const int wide_m = (int)(p.pt / per), wide_n = (int)(p.px / per);   // with the zeros up to the pitch
-  float* const da = reinterpret_cast<float*>(w + p.da);
-  float* const db = reinterpret_cast<float*>(w + p.db);
+  constexpr int per = KIND == MM_PARTS2 ? 4 : 2;
+  const int wide_m = p.kt / per;                          // columns of m, with the zeros behind them
+  const int rows = turned ? p.n : p.m, cols = turned || SQUARE ? p.m : p.n;
+  const int pt = (int)p.pt, px = (int)p.px, pm = (int)p.pm;
+
+  // Buffers that begin at the tile's first row (`back`: at its first column's row)
+  const int pd = SQUARE || turned ? pt : px;
+  const auto to = rows_from(w + (PROD == PROD_GRAM ? p.a : PROD == PROD_POLY ? p.b : p.x), m0, pd);
+  const auto back = rows_from(w + (PROD == PROD_GRAM ? p.a : PROD == PROD_POLY ? p.b : p.xt[a.from ^ 1]), n0, pt);
+  const auto in = rows_from(w + (PROD == PROD_POLY ? p.a : turned ? p.xt[a.from] : p.x), m0, pd);
+  const auto xm = rows_from(w + p.xm, turned ? n0 : m0, pm);
+  const auto da = rows_from(w + p.da, 0, 0), db = rows_from(w + p.db, 0, 0);
+
+  constexpr bool STEPPING = PROD == PROD_STEP || PROD == PROD_LAST;
+  struct Inputs {               // of a round: four neighbours
+    Four<KIND> e;               // of A or X
+    mm_f32x4 x;                 // of the fp32 X
+    mm_f32x4 dj;                // of the diagonal, at the columns
+    float di;                   // and at the row
+    float w[4];
+  };
+  auto load = [&](int b, Inputs (&q)[Tile::ROUNDS]) {
+    const int lj = tile.wn + (b % Tile::TN) * 32 + tile.col(), j = n0 + lj;
 #pragma unroll
-  for (int ti = 0; ti < Tile::TM; ++ti)
+    for (int r = 0; r < Tile::ROUNDS; ++r) {
+      const int li = tile.wm + (b / Tile::TN) * 32 + tile.row(r), i = m0 + li;
+      // (four that begin inside may pass the last: zeros)
+      const bool ok = i < rows && j < cols;
+      if constexpr (PROD == PROD_POLY || (STEPPING && KIND == MM_PARTS2))
+        q[r].e.load(in, ok ? (unsigned)(li * pd) + across<KIND>(j) : TILE_OOB);
+      if constexpr (KIND == MM_F16 && PROD != PROD_GRAM) {
+        const auto& d = PROD == PROD_POLY ? da : db;
+        if (PROD == PROD_POLY || !turned) q[r].di = load_f32(d, ok ? (unsigned)i * 4u : TILE_OOB);
+        if (PROD == PROD_POLY || turned)
+          q[r].dj = __builtin_bit_cast(mm_f32x4, __builtin_amdgcn_raw_buffer_load_b128(d, ok ? (unsigned)j * 4u : TILE_OOB, 0, 0));
+      }
+      if constexpr (KIND == MM_F16 && STEPPING) {
+        if (turned) {
 #pragma unroll
-    for (int tj = 0; tj < Tile::TN; ++tj) {
-      const int j = n0 + wn + tj * 32 + (lane & 31);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int i = m0 + wm + ti * 32 + 8 * q + 4 * (lane >> 5);    // the first of four rows
-        float v[4];
-        if constexpr (PROD == PROD_GRAM || PROD == PROD_POLY) {
-          char* const C = w + (PROD == PROD_GRAM ? p.a : p.b);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            float x = acc[ti][tj][4 * q + c] * PER_UNIT;
-            const bool in = i + c < p.m && j < p.m;
-            if constexpr (PROD == PROD_POLY) {
-              const float e = in ? get_value<KIND>(w + p.a, place<KIND>(i + c, j, p.pt)) : 0.f;
-              if constexpr (KIND == MM_F16) {
-                const float di = in ? da[i + c] : 0.f, dj = in ? da[j] : 0.f;
-                // (D + F)^2, F without a diagonal
-                x = i + c == j ? fmaf(di * PER_UNIT, di, x) : fmaf((di + dj) * PER_UNIT, e, x);
-                x = fmaf(NS_C, x, NS_B * (i + c == j ? di : e));
-              } else {
-                x = fmaf(NS_C, x, NS_B * e);
-              }
-            }
-            if constexpr (KIND == MM_F16) {
-              if (i + c == j) {
-                if (in) (PROD == PROD_GRAM ? da : db)[j] = x;
-                x = 0.f;
-              }
-            }
-            v[c] = in ? x : 0.f;
-            if (i + c < p.m && j < wide_m) put_value<KIND>(C, place<KIND>(i + c, j, p.pt), v[c]);
-          }
-          if (bx != by && j < p.m && i < wide_m) put_four<KIND>(C, place<KIND>(j, i, p.pt), v);
-        } else if (PROD == PROD_LAST && a.turned) {
-          // rows of X^T down, rows of B across
-          float4 four = make_float4(0.f, 0.f, 0.f, 0.f);
-          if constexpr (KIND == MM_F16)
-            if (j < p.m && i < wide_n) four = *reinterpret_cast<const float4*>(w + p.xm + j * p.pm + (int64_t)i * 4);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            if (i + c >= p.n || j >= p.m) continue;
-            float x;
-            if constexpr (KIND == MM_PARTS2) {
-              const float e = get_value<KIND>(w + p.xt[a.from], place<KIND>(i + c, j, p.pt));
-              x = fmaf(NS_A, e, acc[ti][tj][4 * q + c] * PER_UNIT);
-            } else {
-              const float e = c == 0 ? four.x : c == 1 ? four.y : c == 2 ? four.z : four.w;
-              x = fmaf(NS_A, e, fmaf(db[j] * PER_UNIT, (float)(_Float16)e, acc[ti][tj][4 * q + c] * PER_UNIT));
-            }
-            put_result(a, z, i + c, j, x * PER_UNIT);
-          }
+          for (int c = 0; c < 4; ++c)
+            q[r].x[c] = load_f32(xm, ok && j + c < cols ? (unsigned)((lj + c) * pm + i * 4) : TILE_OOB);
         } else {
+          q[r].x = __builtin_bit_cast(
+              mm_f32x4, __builtin_amdgcn_raw_buffer_load_b128(xm, ok ? (unsigned)(li * pm + j * 4) : TILE_OOB, 0, 0));
+        }
+      }
+      if constexpr (PROD == PROD_LAST)
+        if (a.w && ok) load_user(a.w, a.out_type, z * a.stride_w + i * a.ldw + j, cols - j, q[r].w);
+    }
+  };
+  auto finish = [&](int b, const Inputs (&q)[Tile::ROUNDS]) {
+    const int bi = tile.wm + (b / Tile::TN) * 32, bj = tile.wn + (b % Tile::TN) * 32;
+    const int lj = bj + tile.col(), j = n0 + lj;
+    tile.spread(b);
+    float v[Tile::ROUNDS][4];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const bool in = i + c < p.m && j < p.n;
-            float x = 0.f;
-            if (in) {
-              if constexpr (KIND == MM_PARTS2) {
-                const float e = get_value<KIND>(w + p.x, place<KIND>(i + c, j, p.px));
-                x = fmaf(NS_A, e, acc[ti][tj][4 * q + c] * PER_UNIT);
-              } else {
-                float* const xm = reinterpret_cast<float*>(w + p.xm + (i + c) * p.pm) + j;
-                const float e = *xm;
-                x = fmaf(NS_A, e, fmaf(db[i + c] * PER_UNIT, (float)(_Float16)e, acc[ti][tj][4 * q + c] * PER_UNIT));
-                if constexpr (PROD == PROD_STEP) *xm = x;
-              }
-              if constexpr (PROD == PROD_STEP)
-                put_value<KIND>(w + p.x, place<KIND>(i + c, j, p.px), x);
-              else
-                put_result(a, z, i + c, j, x * PER_UNIT);
-            }
-            v[c] = x;
+    for (int r = 0; r < Tile::ROUNDS; ++r) {
+      tile.template sums<float>(r, v[r]);
+      const int li = bi + tile.row(r), i = m0 + li;
+      const bool ok = i < rows && j < cols;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        float x = v[r][c] * PER_UNIT;
+        if constexpr (PROD == PROD_POLY) {
+          const float e = q[r].e[c];
+          if constexpr (KIND == MM_F16) {
+            const float di = q[r].di;                     // (D + F)^2, F without a diagonal
+            x = i == j + c ? fmaf(di * PER_UNIT, di, x) : fmaf((di + q[r].dj[c]) * PER_UNIT, e, x);
+            x = fmaf(NS_C, x, NS_B * (i == j + c ? di : e));
+          } else {
+            x = fmaf(NS_C, x, NS_B * e);
           }
-          if constexpr (PROD == PROD_STEP)
-            if (j < p.n && i < wide_m) put_four<KIND>(w + p.xt[a.from ^ 1], place<KIND>(j, i, p.pt), v);
+        }
+        if constexpr (SQUARE && KIND == MM_F16) {
+          store_f32(PROD == PROD_GRAM ? da : db, ok && i == j + c ? (unsigned)i * 4u : TILE_OOB, x);
+          if (i == j + c) x = 0.f;
+        }
+        if constexpr (STEPPING) {
+          if constexpr (KIND == MM_PARTS2) {
+            x = fmaf(NS_A, q[r].e[c], x);
+          } else {
+            const float e = q[r].x[c];
+            x = fmaf(NS_A, e, fmaf((turned ? q[r].dj[c] : q[r].di) * PER_UNIT, (float)(_Float16)e, x));
+          }
+        }
+        v[r][c] = ok && j + c < cols ? x : 0.f;           // zeros behind the last
+      }
+      if constexpr (PROD == PROD_LAST) {
+        float y[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          y[c] = v[r][c] * PER_UNIT;
+          if (a.w) y[c] = fmaf(-a.rate, y[c], a.keep * q[r].w[c]);
+        }
+        if (ok) store_user(a.out, a.out_type, z * a.stride_o + i * a.ldo + j, cols - j, y);
+      } else {
+        // (of X the zeros lie there already, from the first)
+        const bool kept = i < rows && j < (SQUARE ? wide_m : cols);
+        store_four<KIND>(to, kept ? (unsigned)(li * pd) + across<KIND>(j) : TILE_OOB, v[r]);
+        if constexpr (PROD == PROD_STEP && KIND == MM_F16) {
+          const mm_f32x4 y = {v[r][0], v[r][1], v[r][2], v[r][3]};
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(mm_u32x4, y), xm, kept ? (unsigned)(li * pm + j * 4) : TILE_OOB, 0, 0);
         }
       }
     }
+    if constexpr (PROD == PROD_LAST) return;
+    if (SQUARE && bx == by) return;
+    if constexpr (G > 1) Tile::meet();                    // a sum's places are other waves' too
+#pragma unroll
+    for (int r = 0; r < Tile::ROUNDS; ++r) tile.put_back(r, v[r]);
+    Tile::meet();
+#pragma unroll
+    for (int r = 0; r < Tile::ROUNDS; ++r) {
+      const int lr = bj + tile.row(r), lc = bi + tile.col();
+      float x[4];
+      tile.crossed(r, x);
+      store_four<KIND>(back, n0 + lr < cols && m0 + lc < wide_m ? (unsigned)(lr * pt) + across<KIND>(m0 + lc) : TILE_OOB, x);
+    }
+  };
+  // a block's inputs are on their way while the block before is finished
+  Inputs q[2][Tile::ROUNDS];
+  load(0, q[0]);
+#pragma unroll
+  for (int b = 0; b < Tile::BLOCKS; ++b) {
+    if (b + 1 < Tile::BLOCKS) load(b + 1, q[(b + 1) & 1]);
+    finish(b, q[b & 1]);
+  }
 }
 
-template <int KIND, int PROD, int BM, int WM, int WN, int NS, int OCC>
+template <int KIND, int PROD, int BM, int WM, int WN, int NS, int G, int OCC>
 hipError_t launch_tile(MmArgs a, int64_t count, hipStream_t s) {
-  const int rows = PROD == PROD_LAST && a.turned ? a.p.n : a.p.m;
-  const int cols = PROD == PROD_LAST && a.turned ? a.p.m : PROD == PROD_STEP || PROD == PROD_LAST ? a.p.n : a.p.m;
+  constexpr bool SQUARE = PROD == PROD_GRAM || PROD == PROD_POLY;
+  const bool turned = PROD == PROD_LAST && a.turned;
+  const int rows = turned ? a.p.n : a.p.m, cols = turned || SQUARE ? a.p.m : a.p.n;
   a.mt = (rows + BM - 1) / BM;
   a.nt = (cols + BM - 1) / BM;
-  a.total = PROD == PROD_GRAM || PROD == PROD_POLY ? a.mt * (a.mt + 1) / 2 : a.mt * a.nt;
-  return launch_k(orth_mm_kernel<KIND, PROD, BM, BM, WM, WN, NS, OCC>, dim3(mm_grid(a.total), (unsigned)count),
-                  dim3((BM / WM) * (BM / WN) * 64), 0, s, a);
+  a.total = SQUARE ? a.mt * (a.mt + 1) / 2 : a.mt * a.nt;
+  return launch_k(orth_mm_kernel<KIND, PROD, BM, BM, WM, WN, NS, G, OCC>, dim3(mm_grid(a.total), (unsigned)count),
+                  dim3((BM / WM) * (BM / WN) * G * 64), 0, s, a);
 }
 
 template <int KIND, int PROD>
 hipError_t launch_product(const MmArgs& a, int64_t count, int units, hipStream_t s) {
-  const int64_t m = a.p.m, n = PROD == PROD_GRAM || PROD == PROD_POLY ? a.p.m : a.p.n;
-  auto tiles = [&](int64_t b) { return count * ((m + b - 1) / b) * ((n + b - 1) / b); };
-  if (tiles(256) >= units) return launch_tile<KIND, PROD, 256, 128, 64, 2, 2>(a, count, s);
-  if (tiles(128) >= units) return launch_tile<KIND, PROD, 128, 64, 64, 2, 2>(a, count, s);
-  return launch_tile<KIND, PROD, 64, 32, 32, 3, 2>(a, count, s);
+  constexpr bool SQUARE = PROD == PROD_GRAM || PROD == PROD_POLY;
+  auto tiles = [&](int64_t b) {
+    const int64_t m = (a.p.m + b - 1) / b, n = (a.p.n + b - 1) / b;
+    return count * (SQUARE ? m * (m + 1) / 2 : m * n);
+  };
+  const int64_t bytes = PROD == PROD_GRAM ? a.p.kx : a.p.kt;
+  switch (mm_shape(tiles, units, (bytes + MM_STAGE - 1) / MM_STAGE)) {
+    case MM_64_GROUPS: return launch_tile<KIND, PROD, 64, 32, 32, 3, 2, 2>(a, count, s);
+    case MM_64: return launch_tile<KIND, PROD, 64, 32, 32, 3, 1, 3>(a, count, s);
+    case MM_128: return launch_tile<KIND, PROD, 128, 64, 32, 2, 1, 4>(a, count, s);
+    case MM_192: return launch_tile<KIND, PROD, 192, 96, 96, 3, 1, 1>(a, count, s);
+    default: return launch_tile<KIND, PROD, 256, 128, 64, 2, 1, 2>(a, count, s);
+  }
 }
 
 struct OrthCall {
@@ -426,6 +537,32 @@ hipError_t orth_run(const OrthCall& c, int units, hipStream_t s) {
   const OrthPlan p = orth_plan(KIND == MM_PARTS2, c.rows, c.cols);
   char* const work = static_cast<char*>(c.work);
   const int64_t ldm = c.cols, stride_m = c.rows * c.cols;
+  if (c.rows <= ORTH_SMALL || c.cols <= ORTH_SMALL) {
+    SmallArgs<T> q{};
+    q.g = {static_cast<const T*>(c.g), c.ldg, c.stride_g};
+    q.m = {c.m, ldm, stride_m};
+    q.m_out = {c.m_out, ldm, stride_m};
+    q.momentum = c.momentum;
+    q.nesterov = c.nesterov;
+    q.turned = c.rows > c.cols;
+    q.work = work;
+    q.p = small_plan(c.rows, c.cols);
+    q.out_type = c.out_type;
+    q.out = c.out;
+    q.ldo = c.ldo;
+    q.stride_o = c.stride_o;
+    q.w = c.w;
+    q.ldw = ldm;
+    q.stride_w = stride_m;
+    q.keep = c.keep;
+    q.rate = c.rate;
+    switch (q.p.mb) {
+      case 1: return launch_small<T, 1>(q, c.count, NS_A, NS_B, NS_C, NF_ORTH_STEPS, s);
+      case 2: return launch_small<T, 2>(q, c.count, NS_A, NS_B, NS_C, NF_ORTH_STEPS, s);
+      case 3: return launch_small<T, 3>(q, c.count, NS_A, NS_B, NS_C, NF_ORTH_STEPS, s);
+      default: return launch_small<T, 4>(q, c.count, NS_A, NS_B, NS_C, NF_ORTH_STEPS, s);
+    }
+  }
   SumArgs<T> u{};
   u.g = {static_cast<const T*>(c.g), c.ldg, c.stride_g};
   u.m = {c.m, ldm, stride_m};
@@ -482,11 +619,11 @@ hipError_t orth_run(const OrthCall& c, int units, hipStream_t s) {
   return hipSuccess;
 }
 
-nf_status check_stack(const char* what, const void* p, int64_t elem, int64_t rows, int64_t cols, int64_t ld) {
+nf_status check_stack(const char* what, const void* p, int64_t elem, int64_t cols, int64_t ld) {
   if (!p) return op_fail(NF_EINVAL, "NULL %s", what);
   if (!op_aligned(p, (uintptr_t)elem)) return op_fail(NF_EINVAL, "%s is not aligned to its elements", what);
-  if (ld < cols) return op_fail(NF_ESHAPE, "%s: the row pitch is smaller than the columns", what);
-  (void)rows;
+  if (ld < cols || ld > NF_ORTH_MAX_LD)
+    return op_fail(NF_ESHAPE, "%s: the row pitch must be at least the columns and at most %d", what, NF_ORTH_MAX_LD);
   return NF_OK;
 }
 
@@ -531,12 +668,13 @@ int64_t nf_orthogonalize_work(int32_t dtype, int64_t count, int64_t rows, int64_
     return -1;
   }
   if (check_sizes(count, rows, cols) != NF_OK) return -1;
-  const OrthPlan p = orth_plan(dtype == NF_F32, rows, cols);
-  if (count > 0 && p.bytes > INT64_MAX / count) {
+  const int64_t one = rows <= ORTH_SMALL || cols <= ORTH_SMALL ? small_plan(rows, cols).bytes
+                                                               : orth_plan(dtype == NF_F32, rows, cols).bytes;
+  if (count > 0 && one > INT64_MAX / count) {
     op_fail(NF_ESHAPE, "the workspace's size does not fit");
     return -1;
   }
-  return p.bytes * count;
+  return one * count;
 }
 
 nf_status nf_orthogonalize(const void* d_x, int32_t dtype, int64_t count, int64_t rows, int64_t cols, int64_t ld,
@@ -547,8 +685,8 @@ nf_status nf_orthogonalize(const void* d_x, int32_t dtype, int64_t count, int64_
   if (need < 0) return op_float_type(dtype) && dtype != NF_F16 ? (count < 0 || rows < 1 || cols < 1 ? NF_EINVAL : NF_ESHAPE) : NF_EINVAL;
   if (count == 0) return NF_OK;
   const int64_t e = op_size(dtype);
-  nf_status st = check_stack("the matrices", d_x, e, rows, cols, ld);
-  if (st == NF_OK) st = check_stack("the result", d_out, e, rows, cols, ld_out);
+  nf_status st = check_stack("the matrices", d_x, e, cols, ld);
+  if (st == NF_OK) st = check_stack("the result", d_out, e, cols, ld_out);
   if (st == NF_OK) st = check_work(d_work, work_bytes, need);
   if (st != NF_OK) return st;
   if (count > 1 && (stride < 0 || stride_out < (rows - 1) * ld_out + cols))
@@ -585,11 +723,11 @@ nf_status nf_muon_step(const void* d_w, int32_t w_dtype, const float* d_m, const
   const int64_t need = nf_orthogonalize_work(w_dtype, count, rows, cols);
   if (need < 0) return NF_ESHAPE;
   if (count == 0) return NF_OK;
-  st = check_stack("the weights", d_w, op_size(w_dtype), rows, cols, cols);
-  if (st == NF_OK) st = check_stack("the momentum", d_m, 4, rows, cols, cols);
-  if (st == NF_OK) st = check_stack("the gradient", d_g, op_size(g_dtype), rows, cols, cols);
-  if (st == NF_OK) st = check_stack("the new weights", d_w_out, op_size(w_dtype), rows, cols, cols);
-  if (st == NF_OK) st = check_stack("the new momentum", d_m_out, 4, rows, cols, cols);
+  st = check_stack("the weights", d_w, op_size(w_dtype), cols, cols);
+  if (st == NF_OK) st = check_stack("the momentum", d_m, 4, cols, cols);
+  if (st == NF_OK) st = check_stack("the gradient", d_g, op_size(g_dtype), cols, cols);
+  if (st == NF_OK) st = check_stack("the new weights", d_w_out, op_size(w_dtype), cols, cols);
+  if (st == NF_OK) st = check_stack("the new momentum", d_m_out, 4, cols, cols);
   if (st == NF_OK) st = check_work(d_work, work_bytes, need);
   if (st != NF_OK) return st;
   const int64_t all = count * rows * cols;

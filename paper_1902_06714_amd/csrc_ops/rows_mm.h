@@ -63,18 +63,14 @@ struct StageLoader {
       off[i] = (unsigned)at * (unsigned)m.pitch + (unsigned)(((lane & 7) ^ (lane >> 3)) << 4);
     }
   }
-  // stage at byte k0; `left` bytes of k from there (a lane whose piece lies past
-  // them loads zeros: its offset lies past the buffer)
-  template <bool TAIL>
-  __device__ __forceinline__ void load(unsigned lds, int k0, int left, int wave, int lane) const {
-    const bool in = !TAIL || (((lane & 7) ^ (lane >> 3)) << 4) < left;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const unsigned o = in ? off[i] + (unsigned)k0 : TILE_OOB;
-      const unsigned to = __builtin_amdgcn_readfirstlane(lds + (i * NW + wave) * 1024);
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(o), "s"(rsrc)
-                   : "memory", "m0");
-    }
+  // load i of a stage at byte k0 (a multiple of 128); `in`: whether the lane's piece
+  // lies inside the operand's bytes (else its offset lies past the buffer and it
+  // loads zeros)
+  __device__ __forceinline__ void load(int i, unsigned lds, int k0, bool in, int wave) const {
+    const unsigned to = __builtin_amdgcn_readfirstlane(lds + (i * NW + wave) * 1024);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to),
+                 "v"(in ? off[i] : TILE_OOB), "s"(rsrc), "s"(k0)
+                 : "memory", "m0");
   }
 };
 
@@ -91,30 +87,62 @@ __device__ __forceinline__ void mm_product(mm_f32x16& c, const mm_i32x4& a, cons
   c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-// A tile of BM rows of A by BN rows of B, by waves of WM x WN; NS stages in LDS.
-// Afterwards register v of acc[i][j] of a lane holds row
-// wm + 32 i + 8 (v / 4) + 4 (lane / 32) + v % 4 and column wn + 32 j + lane % 32.
-template <int KIND, int BM, int BN, int WM, int WN, int NS>
+// A tile of BM rows of A by BN rows of B, by G groups of waves of WM x WN, each on
+// its share of k; NS stages of each group in LDS.
+//
+// Stage t lies in buffer t % NS.  A step is 32 bytes of k of every row (64 of
+// pairs of parts); its operands are read from LDS while the step before is
+// multiplied, so a wave alone on its SIMD keeps the matrix pipe busy.  Before the
+// last step of a stage the waves meet: by then each has read all of stage t, whose
+// buffer stage t + NS is requested into, and waited for its own loads of stage
+// t + 1, which all may read after.
+//
+// A launch of few tiles runs at the pace at which a compute unit takes in a tile's
+// operands (105 GB/s here, whatever the waves' shares: 0.16 us for a stage of 64 x 64, of f16
+// and of pairs alike); one group of waves reaches 0.25 - 0.28, two 0.17 - 0.21.
+//
+// Afterwards a wave's blocks of 32 x 32 sums go through LDS, so that a lane has
+// four neighbours of a row and memory is read and written in whole lines.
+constexpr int MM_PITCH = 36;                        // words of a column of a block in LDS
+constexpr int MM_BLOCK = 32 * MM_PITCH * 4;         // bytes of a block in LDS
+
+template <int KIND, int BM, int BN, int WM, int WN, int NS, int G>
 struct MmTile {
-  static constexpr int NW = (BM / WM) * (BN / WN), THREADS = NW * 64;
-  static constexpr int TM = WM / 32, TN = WN / 32;
-  static constexpr int STAGE = (BM + BN) * MM_STAGE, LDS = NS * STAGE;
+  static constexpr int NW = (BM / WM) * (BN / WN), THREADS = NW * G * 64;
+  static constexpr int TM = WM / 32, TN = WN / 32, BLOCKS = TM * TN;
+  static constexpr int STAGE = (BM + BN) * MM_STAGE, LDS = G * NS * STAGE;
+  static constexpr int STEPS = KIND == MM_PARTS2 ? 2 : 4;   // of a stage
+  static constexpr int P = KIND == MM_PARTS2 ? 2 : 1;       // parts of a value
+  static constexpr int ROUNDS = 4 / G;                      // of 8 rows of a block that a wave finishes
   typedef typename MmAcc<KIND>::type Acc;
   typedef StageLoader<BM, NW> LA;
   typedef StageLoader<BN, NW> LB;
   static constexpr int PER = LA::N + LB::N;     // a wave's loads of a stage
+  static_assert(NS >= 2 && (NS - 1) * PER < 64, "loads that the counter can hold");
+  static_assert(G * NW * MM_BLOCK <= LDS, "a block of each wave in LDS");
+  static_assert(G == 1 || G == 2 || G == 4, "whole rounds");
 
-  __device__ __forceinline__ static void run(const MmRows& A, const MmRows& B, int bytes, int m0, int n0,
-                                             char* lds, Acc (&acc)[TM][TN]) {
-    const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = (wave % (BM / WM)) * WM, wn = (wave / (BM / WM)) * WN;
+  int lane, wave, group;                        // wave: of the group
+  int wm, wn;                                   // the wave's place in the tile
+  char* lds;
+  Acc acc[TM][TN];
+
+  __device__ __forceinline__ void run(const MmRows& A, const MmRows& B, int bytes, int m0, int n0, char* shared) {
+    lane = threadIdx.x & 63;
+    const int all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    group = G == 1 ? 0 : all / NW;
+    wave = G == 1 ? all : all % NW;
+    wm = (wave % (BM / WM)) * WM;
+    wn = (wave / (BM / WM)) * WN;
+    lds = shared;
     LA la;
     LB lb;
     la.init(A, m0, wave, lane);
     lb.init(B, n0, wave, lane);
-    const unsigned base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
-    const int stages = (bytes + MM_STAGE - 1) / MM_STAGE;
+    const int stages = ((bytes + MM_STAGE - 1) / MM_STAGE + G - 1) / G;      // of each group
+    const int kbeg = group * stages * MM_STAGE, kend = min(bytes, kbeg + stages * MM_STAGE);
+    char* const mine = lds + group * (NS * STAGE);
+    const unsigned base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)mine;
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -122,76 +150,150 @@ struct MmTile {
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[i][j][v] = 0;
 
-    auto request = [&](int t, int buf) {
-      const int k0 = t * MM_STAGE, left = bytes - k0;
+    // load i of stage t.  Behind the last stage it is of no bytes and loads zeros,
+    // so that the number of loads behind a stage's own stays the same.
+    auto request = [&](int i, int t, int buf, bool in) {
       const unsigned to = base + buf * STAGE;
-      if (left >= MM_STAGE) {
-        la.template load<false>(to, k0, left, wave, lane);
-        lb.template load<false>(to + BM * MM_STAGE, k0, left, wave, lane);
-      } else {
-        la.template load<true>(to, k0, left, wave, lane);
-        lb.template load<true>(to + BM * MM_STAGE, k0, left, wave, lane);
-      }
+      const int k0 = __builtin_amdgcn_readfirstlane(min(kbeg + t * MM_STAGE, bytes));
+      if (i < LA::N) la.load(i, to, k0, in, wave);
+      else lb.load(i - LA::N, to + BM * MM_STAGE, k0, in, wave);
     };
+    const int piece = ((lane & 7) ^ (lane >> 3)) << 4;        // of a lane's loads
+    auto inside = [&](int t) { return piece < kend - kbeg - t * MM_STAGE; };
     int at[4];                                  // places of pieces 2 s + lane / 32 in a lane's row
 #pragma unroll
     for (int s = 0; s < 4; ++s) at[s] = ((2 * s + (lane >> 5)) ^ (lane & 7)) << 4;
     const int ra = (wm + (lane & 31)) * MM_STAGE, rb = (BM + wn + (lane & 31)) * MM_STAGE;
-    auto multiply = [&](int buf) {
-      const char* const p = lds + buf * STAGE;
-      auto frag = [&](int row, int s) {
-        return *reinterpret_cast<const mm_i32x4*>(p + row + at[s]);
-      };
-      if constexpr (KIND == MM_PARTS2) {
+    mm_i32x4 a[2][TM][P], b[2][TN][P];
+    auto fetch = [&](int set, int buf, int s) {
+      const char* const p = mine + buf * STAGE;
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          mm_i32x4 a[TM][2], b[TN][2];
+      for (int q = 0; q < P; ++q) {
 #pragma unroll
-          for (int q = 0; q < 2; ++q) {
+        for (int i = 0; i < TM; ++i)
+          a[set][i][q] = *reinterpret_cast<const mm_i32x4*>(p + ra + i * 32 * MM_STAGE + at[s + 2 * q]);
 #pragma unroll
-            for (int i = 0; i < TM; ++i) a[i][q] = frag(ra + i * 32 * MM_STAGE, s + 2 * q);
+        for (int j = 0; j < TN; ++j)
+          b[set][j][q] = *reinterpret_cast<const mm_i32x4*>(p + rb + j * 32 * MM_STAGE + at[s + 2 * q]);
+      }
+    };
+    constexpr int NM = (P == 2 ? 3 : 1) * TM * TN;      // products of a step
+    // products n0 .. n1 - 1 of a step, f(n) behind product n
+    auto multiply = [&](int set, int n0, int n1, auto&& f) {
 #pragma unroll
-            for (int j = 0; j < TN; ++j) b[j][q] = frag(rb + j * 32 * MM_STAGE, s + 2 * q);
-          }
-#pragma unroll
-          for (int x = 0; x < 3; ++x)
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-              for (int j = 0; j < TN; ++j) mm_product(acc[i][j], a[i][x == 1], b[j][x == 0]);
-        }
-      } else {
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-          mm_i32x4 a[TM], b[TN];
-#pragma unroll
-          for (int i = 0; i < TM; ++i) a[i] = frag(ra + i * 32 * MM_STAGE, s);
-#pragma unroll
-          for (int j = 0; j < TN; ++j) b[j] = frag(rb + j * 32 * MM_STAGE, s);
-#pragma unroll
-          for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j) mm_product(acc[i][j], a[i], b[j]);
-        }
+      for (int n = n0; n < n1; ++n) {
+        const int x = n / (TM * TN), i = n % (TM * TN) / TN, j = n % TN;
+        mm_product(acc[i][j], a[set][i][P == 2 && x == 1], b[set][j][P == 2 && x == 0]);
+        f(n);
       }
     };
 
-    // stage t lies in buffer t % NS; while it is multiplied, the next NS - 1 are on their way.
-    // Behind the last stage each request is of no bytes: it loads zeros, and a
-    // wait for the loads after a stage's own is a wait for the stage.
 #pragma unroll
-    for (int t = 0; t < NS - 1; ++t) request(t, t);
+    for (int t = 0; t < NS; ++t) {
+      const bool in = inside(t);
+#pragma unroll
+      for (int i = 0; i < PER; ++i) request(i, t, t, in);
+    }
+    wait_loads<(NS - 1) * PER>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    fetch(0, 0, 0);
     int buf = 0;
     for (int t = 0; t < stages; ++t) {
-      wait_loads<(NS - 2) * PER>();
-      __builtin_amdgcn_s_barrier();             // everyone's loads of t are here, everyone's reads of t - 1 done
-      asm volatile("" ::: "memory");
-      request(t + NS - 1, (buf + NS - 1) % NS);
-      multiply(buf);
-      buf = buf + 1 == NS ? 0 : buf + 1;
+      const int next = buf + 1 == NS ? 0 : buf + 1;
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) {
+        constexpr int HALF = NM / 2;
+        if (s + 1 < STEPS) {
+          fetch((s + 1) & 1, buf, s + 1);
+          __builtin_amdgcn_sched_barrier(0);
+          multiply(s & 1, 0, NM, [](int) {});
+        } else {
+          multiply(s & 1, 0, HALF, [](int) {});
+          __builtin_amdgcn_sched_barrier(0);
+          wait_loads<(NS - 2) * PER>();
+          __builtin_amdgcn_s_barrier();
+          asm volatile("" ::: "memory");
+          fetch(0, next, 0);
+          __builtin_amdgcn_sched_barrier(0);
+          const bool in = inside(t + NS);
+          // the loads between the products, as evenly as they go
+          multiply(s & 1, HALF, NM, [&](int n) {
+#pragma unroll
+            for (int i = (n - HALF) * PER / (NM - HALF); i < (n + 1 - HALF) * PER / (NM - HALF); ++i) {
+              __builtin_amdgcn_sched_barrier(0);
+              request(i, t + NS, buf, in);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+          });
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      buf = next;
     }
     wait_loads<0>();                            // nothing may write LDS after the tile
     __syncthreads();
+  }
+
+  // What a block in LDS needs between writing and reading: the groups meet, a
+  // wave alone only keeps its own order.
+  __device__ __forceinline__ static void meet() {
+    if constexpr (G > 1) {
+      __syncthreads();
+    } else {
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+  __device__ __forceinline__ int* block_of(int g) const {
+    return reinterpret_cast<int*>(lds + (g * NW + wave) * MM_BLOCK);
+  }
+  // the row of the block, and the first of its four columns, that a lane has in a round
+  __device__ __forceinline__ int row(int round) const { return (group * ROUNDS + round) * 8 + (lane >> 3); }
+  __device__ __forceinline__ int col() const { return (lane & 7) * 4; }
+
+  // A block's sums: register v of a lane is row 8 (v / 4) + 4 (lane / 32) + v % 4 of
+  // column lane % 32.  In LDS they lie by column.
+  __device__ __forceinline__ void spread(int b) {
+    int* const p = block_of(group) + (lane & 31) * MM_PITCH + 4 * (lane >> 5);
+    const Acc& c = acc[b / TN][b % TN];
+    meet();                                     // what was read of the block before
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      mm_i32x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const auto x = c[4 * q + e];            // (a cast of the element itself takes the vector's first)
+        v[e] = __builtin_bit_cast(int, x);
+      }
+      *reinterpret_cast<mm_i32x4*>(p + 8 * q) = v;
+    }
+    meet();
+  }
+  template <class S>
+  __device__ __forceinline__ void sums(int round, S (&x)[4]) const {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[e] = S(0);
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+        x[e] += __builtin_bit_cast(S, block_of(g)[(col() + e) * MM_PITCH + row(round)]);
+    }
+  }
+  // values of the block back into LDS, and four of a column as neighbours: element
+  // (col() + e, row(round)) of the block
+  __device__ __forceinline__ void put_back(int round, const float (&x)[4]) const {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      block_of(0)[(col() + e) * MM_PITCH + row(round)] = __builtin_bit_cast(int, x[e]);
+  }
+  __device__ __forceinline__ void crossed(int round, float (&x)[4]) const {
+    const mm_i32x4 v = *reinterpret_cast<const mm_i32x4*>(block_of(0) + row(round) * MM_PITCH + col());
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int y = v[e];
+      x[e] = __builtin_bit_cast(float, y);
+    }
   }
 };
 
@@ -216,6 +318,33 @@ __device__ __forceinline__ bool mm_place_lower(int total, int& bx, int& by) {
   bx = r;
   by = b - r * (r + 1) / 2;
   return true;
+}
+
+// The tile of a product: tiles(B) of B x B on a card of `units` compute units.
+// Measured (us; X' = a X + B X of m x m in pairs of parts, and in one f16 where two are given):
+//   m       64, two groups   64, one     128         256
+//   768     11.0 / 9.1       11.3 / 9.1  23.0 / 14.4 60.1 / 31.1    144 tiles of 64
+//   1024    13.4 / 10.0      14.5 / 10.6 27.8 / 17.2 74.1 / 35.8    256
+//   1400    31.6 / 19.3      28.6 / 16.0 36.5 / 21.7 94.9 / 43.0    484
+//   2048    81.7 / 43.7      76.8 / 40.0 61.2 / 32.7 131 / 56.7     1024
+//   4096                     471         389         348            (192: 427)
+// and X X^T of 4096 with half the tiles: 128 262, 192 208, 256 245.  The larger three go by
+// the rounds that their tiles make (two of 128 share a compute unit) times a tile's
+// entries times its stages and 6 for its end; a stage of the smaller ones takes 1.1 and 1.2
+// times as long for its entries, and the end of one of 128 runs beside another's stages
+// (8-bit products of 10000 x 1024 over 7 stages: 128 25.3, 256 28.0; 8192 x 4096 over 32: 174, 143).
+enum MmShape { MM_64_GROUPS, MM_64, MM_128, MM_192, MM_256 };
+template <class F>
+inline MmShape mm_shape(F&& tiles, int64_t units, int64_t stages) {
+  const int64_t small = tiles(64);
+  if (small <= units) return MM_64_GROUPS;
+  if (small <= 3 * units) return MM_64;
+  auto cost = [&](int64_t b, int64_t at_once, double stage, double end) {
+    return (double)((tiles(b) + at_once - 1) / at_once) * (double)(at_once / units * b * b) * (stage * (double)stages + end);
+  };
+  const double c128 = cost(128, 2 * units, 1.2, 3.6), c192 = cost(192, units, 1.1, 6.0), c256 = cost(256, units, 1.0, 6.0);
+  if (c256 <= c192 && c256 <= c128) return MM_256;
+  return c192 < c128 ? MM_192 : MM_128;
 }
 inline unsigned mm_grid(int64_t total) { return (unsigned)(8 * ((total + 7) / 8)); }
 

@@ -417,29 +417,38 @@ def nf_calib_spin(us: float, stream=None) -> None:
 # -- operators on the caller's own tensors ------------------------------------
 # Matrices are 2-D (stacks 3-D) GPU tensors whose rows are contiguous; vectors
 # are contiguous.  Outputs are the caller's tensors; None leaves one out.
-NF_TOP_MAX, NF_ORTH_MAX, NF_ORTH_STEPS, NF_LINEAR_I8_MAX, NF_NO_ACT = 64, 65536, 5, 131071, -1
-_elems = {}
+NF_TOP_MAX, NF_ORTH_MAX, NF_ORTH_MAX_LD, NF_ORTH_STEPS = 64, 65536, 1 << 20, 5
+NF_LINEAR_I8_MAX, NF_NO_ACT = 131071, -1
+try:
+    _f32_t, _i32_t, _i64_t, _i8_t = torch.float32, torch.int32, torch.int64, torch.int8
+    _elems = {torch.float32: NF_F32, torch.bfloat16: NF_BF16, torch.float16: NF_F16}
+    _device = torch._C._cuda_getDevice
+    _raw_stream = torch._C._cuda_getCurrentRawStream
+except (NameError, AttributeError):     # no torch, or one without a GPU: no tensor passes the checks
+    _f32_t = _i32_t = _i64_t = _i8_t = None
+    _elems = {}
+
+
+def _tensor(t, name: str):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor on the GPU")
+    return t
 
 
 def _elem(t, name: str) -> int:
     """nf_dtype of a GPU tensor on the current device."""
-    import torch
-    if not _elems:
-        _elems.update({torch.float32: NF_F32, torch.bfloat16: NF_BF16, torch.float16: NF_F16})
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a torch tensor on the GPU")
-    code = _elems.get(t.dtype)
+    code = _elems.get(_tensor(t, name).dtype)
     if code is None or not t.is_cuda:
         raise ValueError(f"{name} must be an fp32, bf16 or fp16 GPU tensor")
-    if t.get_device() != torch.cuda.current_device():
+    if t.get_device() != _device():
         raise ValueError(f"{name} is not on the current device")
     return code
 
 
 def _matrix(t, name: str, shape=None):
     """(pointer, rows, columns, row pitch) of a 2-D tensor of contiguous rows."""
-    if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
-        raise ValueError(f"{name} must be 2-D" + (f" of shape {shape}" if shape else ""))
+    if t.dim() != 2 or (shape is not None and t.shape != shape):
+        raise ValueError(f"{name} must be 2-D" + (f" of shape {tuple(shape)}" if shape else ""))
     rows, cols = t.shape
     ld, one = t.stride()
     if rows <= 1:
@@ -453,32 +462,28 @@ def _vector(t, name: str, dtype, shape):
     """Pointer of a contiguous GPU tensor of this type and shape, None for None."""
     if t is None:
         return None
-    import torch
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a torch tensor on the GPU")
-    if t.dtype != dtype or not t.is_cuda or tuple(t.shape) != shape or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} GPU tensor of shape {shape}")
+    if _tensor(t, name).dtype is not dtype or not t.is_cuda or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} GPU tensor of shape {tuple(shape)}")
     return t.data_ptr()
 
 
 def _queue(stream):
     if stream is not None:
         return _stream(stream)
-    import torch
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None
+    return _raw_stream(_device()) or None
 
 
 def _workspace(work, need: int, stream, name: str):
     """(pointer, bytes, tensor) of the caller's workspace, or of one from torch's
     allocator, which keeps it until the stream has passed the call."""
-    import torch
     if need < 0:
         raise NfError(NF_ESHAPE, name)
     if work is None:
         work = torch.empty(need, dtype=torch.uint8, device="cuda")
         if stream is not None:
             work.record_stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
-    elif not isinstance(work, torch.Tensor) or not work.is_cuda or not work.is_contiguous():
+        return work.data_ptr(), need, work
+    if not _tensor(work, "work").is_cuda or not work.is_contiguous():
         raise ValueError("work must be a contiguous GPU tensor")
     return work.data_ptr(), work.numel() * work.element_size(), work
 
@@ -487,23 +492,23 @@ def nf_logprobs(logits, targets=None, logp=None, entropy=None, stat=None, top_id
                 scale: float = 1.0, stream=None) -> None:
     """logits [rows][classes], targets [rows] int64; logp, entropy [rows], stat
     [rows][2], top_ids (int32) and top_logp [rows][n_top] receive what they name."""
-    import torch
     code = _elem(logits, "logits")
     x, rows, cols, ld = _matrix(logits, "logits")
-    f = torch.float32
     top = top_ids if top_ids is not None else top_logp
     n_top = 0 if top is None else top.shape[-1]
-    _check(_lib.nf_logprobs(x, code, rows, cols, ld, scale, _vector(targets, "targets", torch.int64, (rows,)),
-                            n_top, _vector(logp, "logp", f, (rows,)), _vector(entropy, "entropy", f, (rows,)),
-                            _vector(stat, "stat", f, (rows, 2)),
-                            _vector(top_ids, "top_ids", torch.int32, (rows, n_top)),
-                            _vector(top_logp, "top_logp", f, (rows, n_top)), _queue(stream)), "nf_logprobs")
+    row = (rows,)
+    st = _lib.nf_logprobs(x, code, rows, cols, ld, scale, _vector(targets, "targets", _i64_t, row), n_top,
+                          _vector(logp, "logp", _f32_t, row), _vector(entropy, "entropy", _f32_t, row),
+                          _vector(stat, "stat", _f32_t, (rows, 2)), _vector(top_ids, "top_ids", _i32_t, (rows, n_top)),
+                          _vector(top_logp, "top_logp", _f32_t, (rows, n_top)), _queue(stream))
+    if st:
+        raise NfError(st, "nf_logprobs")
 
 
 def _like(t, of, code: int, name: str):
     if _elem(t, name) != code:
         raise ValueError(f"{name} must have the type of the logits")
-    p, _, _, ld = _matrix(t, name, tuple(of.shape))
+    p, _, _, ld = _matrix(t, name, of.shape)
     return p, ld
 
 
@@ -511,31 +516,31 @@ def nf_logprobs_train(logits, targets, g_logp, g_entropy, dlogits, logp=None, en
                       scale: float = 1.0, stream=None) -> None:
     """nf_logprobs with the gradient of sum(g_logp logp + g_entropy entropy) in
     dlogits [rows][classes], which may be the logits."""
-    import torch
     code = _elem(logits, "logits")
     x, rows, cols, ld = _matrix(logits, "logits")
     dx, ldd = _like(dlogits, logits, code, "dlogits")
-    f = torch.float32
-    _check(_lib.nf_logprobs_train(x, code, rows, cols, ld, scale, _vector(targets, "targets", torch.int64, (rows,)),
-                                  _vector(g_logp, "g_logp", f, (rows,)),
-                                  _vector(g_entropy, "g_entropy", f, (rows,)), _vector(logp, "logp", f, (rows,)),
-                                  _vector(entropy, "entropy", f, (rows,)), _vector(stat, "stat", f, (rows, 2)),
-                                  dx, ldd, _queue(stream)), "nf_logprobs_train")
+    row = (rows,)
+    st = _lib.nf_logprobs_train(x, code, rows, cols, ld, scale, _vector(targets, "targets", _i64_t, row),
+                                _vector(g_logp, "g_logp", _f32_t, row), _vector(g_entropy, "g_entropy", _f32_t, row),
+                                _vector(logp, "logp", _f32_t, row), _vector(entropy, "entropy", _f32_t, row),
+                                _vector(stat, "stat", _f32_t, (rows, 2)), dx, ldd, _queue(stream))
+    if st:
+        raise NfError(st, "nf_logprobs_train")
 
 
 def nf_logprobs_grad(logits, targets, stat, entropy, g_logp, g_entropy, dlogits, scale: float = 1.0,
                      stream=None) -> None:
     """The same gradient from the stat (and entropy) of an earlier nf_logprobs."""
-    import torch
     code = _elem(logits, "logits")
     x, rows, cols, ld = _matrix(logits, "logits")
     dx, ldd = _like(dlogits, logits, code, "dlogits")
-    f = torch.float32
-    _check(_lib.nf_logprobs_grad(x, code, rows, cols, ld, scale, _vector(targets, "targets", torch.int64, (rows,)),
-                                 _vector(stat, "stat", f, (rows, 2)), _vector(entropy, "entropy", f, (rows,)),
-                                 _vector(g_logp, "g_logp", f, (rows,)),
-                                 _vector(g_entropy, "g_entropy", f, (rows,)), dx, ldd, _queue(stream)),
-           "nf_logprobs_grad")
+    row = (rows,)
+    st = _lib.nf_logprobs_grad(x, code, rows, cols, ld, scale, _vector(targets, "targets", _i64_t, row),
+                               _vector(stat, "stat", _f32_t, (rows, 2)), _vector(entropy, "entropy", _f32_t, row),
+                               _vector(g_logp, "g_logp", _f32_t, row), _vector(g_entropy, "g_entropy", _f32_t, row),
+                               dx, ldd, _queue(stream))
+    if st:
+        raise NfError(st, "nf_logprobs_grad")
 
 
 def _stack(t, name: str):
@@ -578,79 +583,84 @@ def nf_muon_step(w, m, g, w_out, m_out, eta: float, momentum: float = 0.95, nest
                  decay: float = 0.0, work=None, stream=None) -> None:
     """One step on w ([rows][cols] or a stack) with gradient g and fp32 momentum m, into
     w_out and m_out (which may be w and m).  All contiguous."""
-    import torch
     wc, gc = _elem(w, "w"), _elem(g, "g")
-    shape = tuple(w.shape)
-    p, count, rows, cols, _, _ = _stack(w, "w")
-    f = torch.float32
-    wp = _vector(w, "w", w.dtype, shape)
-    gp = _vector(g, "g", g.dtype, shape)
+    shape = w.shape
+    _, count, rows, cols, _, _ = _stack(w, "w")
+    wp, gp = _vector(w, "w", w.dtype, shape), _vector(g, "g", g.dtype, shape)
+    mp, wo = _vector(m, "m", _f32_t, shape), _vector(w_out, "w_out", w.dtype, shape)
+    mo = _vector(m_out, "m_out", _f32_t, shape)
     k, n, keep = _workspace(work, _lib.nf_orthogonalize_work(wc, count, rows, cols), stream, "nf_muon_step")
-    _check(_lib.nf_muon_step(wp, wc, _vector(m, "m", f, shape), gp, gc, count, rows, cols, eta, momentum,
-                             int(nesterov), decay, _vector(w_out, "w_out", w.dtype, shape),
-                             _vector(m_out, "m_out", f, shape), k, n, _queue(stream)), "nf_muon_step")
+    st = _lib.nf_muon_step(wp, wc, mp, gp, gc, count, rows, cols, eta, momentum, int(nesterov), decay, wo, mo, k, n,
+                           _queue(stream))
+    if st:
+        raise NfError(st, "nf_muon_step")
 
 
 def _act(act) -> int:
     return NF_NO_ACT if act is None else ACT_CODES[act] if isinstance(act, str) else int(act)
 
 
-def _bytes_matrix(t, name: str, rows: Optional[int] = None):
-    import torch
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a torch tensor on the GPU")
-    if t.dtype != torch.int8 or not t.is_cuda:
+def _bytes_matrix(t, name: str):
+    if _tensor(t, name).dtype is not _i8_t or not t.is_cuda:
         raise ValueError(f"{name} must be an int8 GPU tensor")
-    p, r, c, ld = _matrix(t, name)
-    if rows is not None and r != rows:
-        raise ValueError(f"{name} must have {rows} rows")
-    return p, r, c, ld
+    return _matrix(t, name)
 
 
 def nf_quantize_rows(x, q, scale, stream=None) -> None:
     """x [rows][cols] into int8 q [rows][cols up to a multiple of 16, or more] and fp32
     scale [rows]."""
-    import torch
     code = _elem(x, "x")
     p, rows, cols, ld = _matrix(x, "x")
-    qp, _, wide, ldq = _bytes_matrix(q, "q", rows)
-    if wide < (cols + 15) // 16 * 16:
-        raise ValueError("q must have x's columns, up to a multiple of 16")
-    _check(_lib.nf_quantize_rows(p, code, rows, cols, ld, qp, ldq, _vector(scale, "scale", torch.float32, (rows,)),
-                                 _queue(stream)), "nf_quantize_rows")
+    qp, qrows, wide, ldq = _bytes_matrix(q, "q")
+    if qrows != rows or wide < (cols + 15) // 16 * 16:
+        raise ValueError("q must have x's rows and columns, these up to a multiple of 16")
+    st = _lib.nf_quantize_rows(p, code, rows, cols, ld, qp, ldq, _vector(scale, "scale", _f32_t, (rows,)),
+                               _queue(stream))
+    if st:
+        raise NfError(st, "nf_quantize_rows")
 
 
 def nf_linear_i8(xq, x_scale, wq, w_scale, y, inputs: int, bias=None, act=None, stream=None) -> None:
     """y [rows][outputs] = act(x_scale w_scale (xq wq^T) + bias) of rows and weights
     as nf_quantize_rows leaves them (int8 [..][inputs up to a multiple of 16])."""
-    import torch
     xp, rows, xw, ldx = _bytes_matrix(xq, "xq")
     wp, outs, ww, ldw = _bytes_matrix(wq, "wq")
     wide = (inputs + 15) // 16 * 16
     if xw < wide or ww < wide:
         raise ValueError("xq and wq must hold the inputs, up to a multiple of 16")
-    f = torch.float32
     yc = _elem(y, "y")
     yp, _, _, ldy = _matrix(y, "y", (rows, outs))
-    _check(_lib.nf_linear_i8(xp, ldx, _vector(x_scale, "x_scale", f, (rows,)), wp, ldw,
-                             _vector(w_scale, "w_scale", f, (outs,)), _vector(bias, "bias", f, (outs,)), _act(act),
-                             rows, inputs, outs, yp, yc, ldy, _queue(stream)), "nf_linear_i8")
+    out = (outs,)
+    st = _lib.nf_linear_i8(xp, ldx, _vector(x_scale, "x_scale", _f32_t, (rows,)), wp, ldw,
+                           _vector(w_scale, "w_scale", _f32_t, out), _vector(bias, "bias", _f32_t, out), _act(act),
+                           rows, inputs, outs, yp, yc, ldy, _queue(stream))
+    if st:
+        raise NfError(st, "nf_linear_i8")
+
+
+def nf_linear_i8_work(rows: int, inputs: int) -> int:
+    """Bytes of nf_linear_i8_dynamic's workspace; raises for sizes it would refuse."""
+    n = _lib.nf_linear_i8_work(rows, inputs)
+    if n < 0:
+        raise NfError(NF_ESHAPE, "nf_linear_i8_work")
+    return n
 
 
 def nf_linear_i8_dynamic(x, wq, w_scale, y, bias=None, act=None, work=None, stream=None) -> None:
     """nf_linear_i8 of the rows x [rows][inputs], which it quantises."""
-    import torch
     code, yc = _elem(x, "x"), _elem(y, "y")
     xp, rows, cols, ldx = _matrix(x, "x")
     wp, outs, ww, ldw = _bytes_matrix(wq, "wq")
     if ww < (cols + 15) // 16 * 16:
         raise ValueError("wq must hold x's columns, up to a multiple of 16")
-    f = torch.float32
     yp, _, _, ldy = _matrix(y, "y", (rows, outs))
+    out = (outs,)
+    ws, bs = _vector(w_scale, "w_scale", _f32_t, out), _vector(bias, "bias", _f32_t, out)
     k, n, keep = _workspace(work, _lib.nf_linear_i8_work(rows, cols), stream, "nf_linear_i8_dynamic")
-    _check(_lib.nf_linear_i8_dynamic(xp, code, ldx, wp, ldw, _vector(w_scale, "w_scale", f, (outs,)),
-                                     _vector(bias, "bias", f, (outs,)), _act(act), rows, cols, outs, yp, yc, ldy,
-                                     k, n, _queue(stream)), "nf_linear_i8_dynamic")
+    st = _lib.nf_linear_i8_dynamic(xp, code, ldx, wp, ldw, ws, bs, _act(act), rows, cols, outs, yp, yc, ldy, k, n,
+                                   _queue(stream))
+    if st:
+        raise NfError(st, "nf_linear_i8_dynamic")
 
 
 def nf_last_error() -> str:
