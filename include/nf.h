@@ -348,12 +348,18 @@ nf_status nf_calib_mfma(int32_t dtype, int64_t iters, void* d_sink, void* stream
  * whose classes are all at minus infinity has log probabilities (and m and log
  * s) of minus infinity and entropy 0.  A row with a NaN or plus infinity gets
  * NaN log probabilities and entropy; NaN ranks above all numbers.
- * rows may be 0. */
+ * rows may be 0.
+ * d_work: nf_logprobs_work(...) bytes aligned to 16 (0 where none is of use, -1
+ * for sizes that the call would refuse), in which few long rows are worked on by
+ * many workgroups each; NULL leaves a row to one.  The sums may then differ in
+ * their last bits. */
 #define NF_TOP_MAX 64
+int64_t nf_logprobs_work(int32_t dtype, int64_t rows, int64_t classes, int32_t n_top,
+                         int32_t gradient);
 nf_status nf_logprobs(const void* d_logits, int32_t dtype, int64_t rows, int64_t classes,
                       int64_t ld, float scale, const int64_t* d_targets, int32_t n_top,
                       float* d_logp, float* d_entropy, float* d_stat, int32_t* d_top_ids,
-                      float* d_top_logp, void* stream);
+                      float* d_top_logp, void* d_work, int64_t work_bytes, void* stream);
 
 /* The gradient with respect to the logits of
  *   sum over rows of g log p_target + h H
@@ -364,14 +370,15 @@ nf_status nf_logprobs(const void* d_logits, int32_t dtype, int64_t rows, int64_t
  * g = -1/rows); nf_logprobs_grad from the d_stat and, with d_g_entropy, the
  * d_entropy of an earlier nf_logprobs on the same logits, targets and scale.
  * d_dlogits: [rows][classes] of the logits' type, ld_d from row to row; it may
- * be the logits' own array with the same pitch, or one apart from it.
+ * be the logits' own array with the same pitch, or one apart from it.  d_work as
+ * above, with n_top 0 and gradient 1.
  * A row without a target has no g.  A target past the last class gives NaN.  A
  * row without probabilities has gradient 0. */
 nf_status nf_logprobs_train(const void* d_logits, int32_t dtype, int64_t rows, int64_t classes,
                             int64_t ld, float scale, const int64_t* d_targets,
                             const float* d_g_logp, const float* d_g_entropy, float* d_logp,
                             float* d_entropy, float* d_stat, void* d_dlogits, int64_t ld_d,
-                            void* stream);
+                            void* d_work, int64_t work_bytes, void* stream);
 nf_status nf_logprobs_grad(const void* d_logits, int32_t dtype, int64_t rows, int64_t classes,
                            int64_t ld, float scale, const int64_t* d_targets,
                            const float* d_stat, const float* d_entropy, const float* d_g_logp,

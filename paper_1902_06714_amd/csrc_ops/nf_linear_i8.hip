@@ -121,14 +121,14 @@ hipError_t launch_quant(const T* x, int64_t ldx, int64_t rows, int cols, int8_t*
   const int vecs = a.wide / Vec16<T>::N;
 #define NF_QUANT(TH, TPR, NV)     \
   if (vecs <= (TPR) * (NV))       \
-    return launch_k(quant_kernel<T, TH, TPR, NV>, dim3((unsigned)((rows + (TH) / (TPR) - 1) / ((TH) / (TPR)))), \
-                    dim3(TH), 0, s, a);
+    return op_launch(quant_kernel<T, TH, TPR, NV>, dim3((unsigned)((rows + (TH) / (TPR) - 1) / ((TH) / (TPR)))), \
+                    dim3(TH), s, a);
   NF_QUANT(256, 64, 1)
   NF_QUANT(256, 64, 4)
   NF_QUANT(256, 256, 2)
   NF_QUANT(256, 256, 8)
 #undef NF_QUANT
-  return launch_k(quant_kernel<T, 1024, 1024, 0>, dim3((unsigned)rows), dim3(1024), 0, s, a);
+  return op_launch(quant_kernel<T, 1024, 1024, 0>, dim3((unsigned)rows), dim3(1024), s, a);
 }
 
 // ---- the product ---------------------------------------------------------------
@@ -241,8 +241,8 @@ hipError_t launch_linear_tile(LinearArgs a, hipStream_t s) {
   a.mt = (a.rows + BM - 1) / BM;
   a.nt = (a.outputs + BM - 1) / BM;
   a.total = a.mt * a.nt;
-  return launch_k(linear_kernel<T, BM, BM, WM, WN, NS, G, OCC>, dim3(mm_grid(a.total)),
-                  dim3((BM / WM) * (BM / WN) * G * 64), 0, s, a);
+  return op_launch(linear_kernel<T, BM, BM, WM, WN, NS, G, OCC>, dim3(mm_grid(a.total)),
+                  dim3((BM / WM) * (BM / WN) * G * 64), s, a);
 }
 
 // ---- few rows: the weights' bytes ----------------------------------------------
@@ -386,7 +386,7 @@ __global__ void __launch_bounds__(64 * FEW_WAVES) linear_few_kernel(const FewArg
 
 template <class X, class T>
 hipError_t launch_few(const FewArgs<X>& f, hipStream_t s) {
-  return launch_k(linear_few_kernel<X, T>, dim3((unsigned)((f.a.outputs + 15) / 16)), dim3(64 * FEW_WAVES), 0, s, f);
+  return op_launch(linear_few_kernel<X, T>, dim3((unsigned)((f.a.outputs + 15) / 16)), dim3(64 * FEW_WAVES), s, f);
 }
 
 // 16 rows are one operand of the matrix instruction; beyond, tiles of 64 x 64 that

@@ -43,6 +43,10 @@ struct LogpArgs {
   int* top_ids;                  // [rows][n_top]
   float* top_logp;
   T* dx;
+  // rows in slices: their number, classes, and what each leaves
+  int slices, slice;
+  float4* part;                  // [rows][slices]: m, sum, sum of exp times d
+  unsigned long long* keys;      // [rows][slices][n_top]
 };
 
 // NaN above all numbers, -0 as 0, and nothing at 0 but places that hold no value
@@ -254,18 +258,21 @@ struct BlockShare {
 };
 
 // NV: 16-byte vectors of the row that a thread holds; 0: none, the row is read
-// anew for each pass over it
-template <class T, int THREADS, int NV, bool GRAD>
+// anew for each pass over it.  PART: a slice of the row, whose sums and
+// alternatives logp_join_kernel puts together.
+template <class T, int THREADS, int NV, bool GRAD, bool PART = false>
 __global__ void __launch_bounds__(THREADS) logp_row_kernel(const LogpArgs<T> a) {
   constexpr int E = Vec16<T>::N, W = THREADS / 64;
   __shared__ BlockShare<W> sh;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t row = blockIdx.x;
-  const T* const x = a.x + row * a.ld;
-  const int V = a.classes;
+  const int64_t row = PART ? blockIdx.y : blockIdx.x;
+  const int start = PART ? (int)blockIdx.x * a.slice : 0;
+  const T* const x = a.x + row * a.ld + start;
+  const int V = PART ? min(a.slice, a.classes - start) : a.classes;
 
   auto load = [&](int j) {           // E values from class j on, minus infinity past the last
     if (j + E <= V) return load16(x + j);
+    // (j may lie past the row altogether)
     Vec16<T> r;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
@@ -311,7 +318,7 @@ __global__ void __launch_bounds__(THREADS) logp_row_kernel(const LogpArgs<T> a) 
       for (; j < V; j += THREADS * E) f(j, load(j));
     }
   };
-  const int64_t t = a.target ? a.target[row] : -1;
+  const int64_t t = !PART && a.target ? a.target[row] : -1;
   float zt = 0.f;
   if (tid == 0 && t >= 0 && t < V) zt = z_of(x[t], a.scale);
 
@@ -340,21 +347,30 @@ __global__ void __launch_bounds__(THREADS) logp_row_kernel(const LogpArgs<T> a) 
     again();
     each([&](int, const Vec16<T>& r) { add(r, m); });
   } else {
-    // running: the sums are relative to the thread's maximum so far
+    // running: the sums are relative to the thread's maximum so far, looked at once
+    // for U vectors (whose places past the row hold minus infinity)
     float run = -__builtin_inff();
     m = 0.f;
-    each([&](int, const Vec16<T>& r) {
-      float c = run;
+    constexpr int U = 4;
+    for (int j = tid * E; j < V; j += U * THREADS * E) {
+      Vec16<T> r[U];
 #pragma unroll
-      for (int e = 0; e < E; ++e) c = fmaxf(c, z_of(r.v[e], a.scale));
+      for (int u = 0; u < U; ++u) r[u] = load(j + u * THREADS * E);
+      float c = -__builtin_inff();
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < E; ++e) c = fmaxf(c, to_float(r[u].v[e]));
+      c = z_of(c, a.scale);
       if (c > run) {
         const float d = run - c, w = exp_of(d);       // run may be minus infinity: s is 0 then
         q = w == 0.f ? 0.f : w * (q + s * d);
         s *= w;
         run = m = c;
       }
-      add(r, m);
-    });
+#pragma unroll
+      for (int u = 0; u < U; ++u) add(r[u], m);
+    }
     const float own = run;
     lane_max = run;
     m = wave_max(run);
@@ -390,7 +406,11 @@ __global__ void __launch_bounds__(THREADS) logp_row_kernel(const LogpArgs<T> a) 
     if (tid == 0) sh.count = 0;
   }
   const RowSums r = row_sums(m, s, q);
-  if (tid == 0) put_row(a, row, r, t, zt);
+  const int64_t piece = PART ? row * a.slices + blockIdx.x : 0;
+  if (tid == 0) {
+    if constexpr (PART) a.part[piece] = make_float4(m, s, q, 0.f);
+    else put_row(a, row, r, t, zt);
+  }
 
   if constexpr (GRAD) {
     const Slope sl = slope_of(a, row, r, t);
@@ -439,18 +459,24 @@ __global__ void __launch_bounds__(THREADS) logp_row_kernel(const LogpArgs<T> a) 
         const float z = z_of(v.v[e], a.scale);
         if (!(z < least) && j + e < V) {         // a NaN too
           const int at = atomicAdd(&sh.count, 1);
-          if (at < TOP_CAP) sh.key[at] = (unsigned long long)ordered(z) << 32 | (unsigned)~(unsigned)(j + e);
+          if (at < TOP_CAP) sh.key[at] = (unsigned long long)ordered(z) << 32 | (unsigned)~(unsigned)(start + j + e);
         }
       }
     });
   __syncthreads();
   const int n = sh.count;
   auto put = [&](int rank, unsigned long long key) {
+    if constexpr (PART) {
+      a.keys[piece * a.n_top + rank] = key;
+      return;
+    }
     const int64_t o = row * a.n_top + rank;
     if (a.top_ids) a.top_ids[o] = (int)~(unsigned)key;
     if (a.top_logp) a.top_logp[o] = log_prob(r, unordered((unsigned)(key >> 32)));
   };
   if (n <= TOP_CAP) {
+    if constexpr (PART)                          // a slice of fewer classes than alternatives
+      for (int k = V + tid; k < a.n_top; k += THREADS) put(k, 0);
     for (int c = tid; c < n; c += THREADS) {
       const unsigned long long key = sh.key[c];
       int rank = 0;
@@ -467,7 +493,7 @@ __global__ void __launch_bounds__(THREADS) logp_row_kernel(const LogpArgs<T> a) 
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const unsigned o = j + e < V ? ordered(z_of(v.v[e], a.scale)) : 0u;
-        const unsigned long long key = (unsigned long long)o << 32 | (unsigned)~(unsigned)(j + e);
+        const unsigned long long key = (unsigned long long)o << 32 | (unsigned)~(unsigned)(start + j + e);
         if (o && (k == 0 || key < last) && key > best) best = key;
       }
     });
@@ -486,13 +512,56 @@ __global__ void __launch_bounds__(THREADS) logp_row_kernel(const LogpArgs<T> a) 
   }
 }
 
+// ---- few long rows: the slices of a row put together -----------------------------
+constexpr int MAX_SLICES = 64;
+constexpr int JOIN_KEYS = 512;       // at most; slices times alternatives
+
+template <class T>
+__global__ void __launch_bounds__(256) logp_join_kernel(const LogpArgs<T> a) {
+  __shared__ unsigned long long key[JOIN_KEYS];
+  __shared__ float sums[3];
+  const int64_t row = blockIdx.x;
+  const int tid = threadIdx.x, n = a.slices * a.n_top;
+  for (int k = tid; k < n; k += 256) key[k] = a.keys[row * n + k];
+  if (tid < 64) {
+    const float4 p = tid < a.slices ? a.part[row * a.slices + tid] : make_float4(0.f, 0.f, 0.f, 0.f);
+    const bool some = p.y != 0.f;    // a NaN too
+    float m = wave_max(some ? p.x : -__builtin_inff());
+    m = m == -__builtin_inff() ? 0.f : m;
+    const float d = p.x - m, w = exp_of(d);
+    const float s = wave_sum(some ? p.y * w : 0.f);
+    const float q = wave_sum(!some ? 0.f : w == 0.f ? 0.f * p.z : w * (p.z + p.y * d));
+    if (tid == 0) {
+      sums[0] = m;
+      sums[1] = s;
+      sums[2] = q;
+    }
+  }
+  __syncthreads();
+  const RowSums r = row_sums(sums[0], sums[1], sums[2]);
+  if (tid == 0) {
+    const int64_t t = a.target ? a.target[row] : -1;
+    put_row(a, row, r, t, t >= 0 && t < a.classes ? z_of(a.x[row * a.ld + t], a.scale) : 0.f);
+  }
+  for (int c = tid; c < n; c += 256) {
+    const unsigned long long own = key[c];
+    if (own == 0) continue;
+    int rank = 0;
+    for (int o = 0; o < n; ++o) rank += key[o] > own;
+    if (rank >= a.n_top) continue;
+    const int64_t o = row * a.n_top + rank;
+    if (a.top_ids) a.top_ids[o] = (int)~(unsigned)own;
+    if (a.top_logp) a.top_logp[o] = log_prob(r, unordered((unsigned)(own >> 32)));
+  }
+}
+
 // ---- the gradient from statistics kept earlier ------------------------------
 template <class T>
 struct GradArgs {
   const T* x;
   T* dx;
   int64_t ld, ld_dx;
-  int64_t rows, blocks;            // blocks of vectors in all
+  int64_t rows;
   int classes, per_row;            // workgroups a row
   float scale;
   const int64_t* target;
@@ -541,6 +610,55 @@ __global__ void __launch_bounds__(256) logp_grad_kernel(const GradArgs<T> a) {
 }
 
 // ---- launches ----------------------------------------------------------------
+// How a call's rows are cut, and where its workspace holds what.
+struct LogpPlan {
+  int slices = 0, slice = 0;     // 0: rows stay whole
+  int64_t keys = 0, stat = 0, entropy = 0, bytes = 0;
+};
+// Few long rows would leave most of the card idle: they are cut so that about 256
+// workgroups have 16 KB or more each.  Another launch or two costs about 4 us each, so rows
+// stay whole below 96 KB, with a gradient below 256 KB (us, cut and whole: see launch_logp).
+LogpPlan logp_plan(int64_t size, int64_t rows, int64_t classes, int n_top, bool grad) {
+  LogpPlan p;
+  const int64_t bytes = classes * size;
+  if (rows < 1 || rows > 64 || bytes < (grad ? 256 : 96) * 1024) return p;
+  int64_t s = 256 / rows;
+  if (s > MAX_SLICES) s = MAX_SLICES;
+  if (s > bytes / 16384) s = bytes / 16384;
+  if (n_top > 0 && s > JOIN_KEYS / n_top) s = JOIN_KEYS / n_top;
+  if (s < 2) return p;
+  p.slice = (int)(((classes + s - 1) / s + 63) / 64 * 64);
+  p.slices = (int)((classes + p.slice - 1) / p.slice);
+  p.keys = rows * p.slices * 16;
+  p.stat = p.keys + rows * p.slices * n_top * 8;
+  p.entropy = p.stat + rows * 8;
+  p.bytes = p.entropy + rows * 4;
+  return p;
+}
+
+template <class T>
+hipError_t launch_parts(LogpArgs<T> a, const LogpPlan& p, char* work, hipStream_t s) {
+  a.slices = p.slices;
+  a.slice = p.slice;
+  a.part = reinterpret_cast<float4*>(work);
+  a.keys = reinterpret_cast<unsigned long long*>(work + p.keys);
+  const dim3 grid((unsigned)p.slices, (unsigned)a.rows);
+  const int64_t vecs = p.slice / Vec16<T>::N;
+  hipError_t e;
+  if (vecs <= 1024) e = op_launch(logp_row_kernel<T, 256, 4, false, true>, grid, dim3(256), s, a);
+  else if (vecs <= 4096) e = op_launch(logp_row_kernel<T, 1024, 4, false, true>, grid, dim3(1024), s, a);
+  else e = op_launch(logp_row_kernel<T, 1024, 0, false, true>, grid, dim3(1024), s, a);
+  if (e != hipSuccess) return e;
+  return op_launch(logp_join_kernel<T>, dim3((unsigned)a.rows), dim3(256), s, a);
+}
+
+template <class T>
+hipError_t launch_grad(GradArgs<T> a, hipStream_t s) {
+  constexpr int64_t per = 256 * Vec16<T>::N * GRAD_VECS;
+  a.per_row = (int)((a.classes + per - 1) / per);
+  return op_launch(logp_grad_kernel<T>, dim3((unsigned)(a.rows * a.per_row)), dim3(256), s, a);
+}
+
 template <class T, bool GRAD>
 hipError_t launch_logp(const LogpArgs<T>& a, int units, hipStream_t s) {
   if (a.classes <= SMALL_MAX) {
@@ -548,7 +666,7 @@ hipError_t launch_logp(const LogpArgs<T>& a, int units, hipStream_t s) {
     auto go = [&](auto g) {
       constexpr int G = decltype(g)::value;
       const int64_t blocks = (a.rows + 256 / G - 1) / (256 / G);
-      return launch_k(logp_small_kernel<T, G, GRAD>, dim3((unsigned)blocks), dim3(256), 0, s, a);
+      return op_launch(logp_small_kernel<T, G, GRAD>, dim3((unsigned)blocks), dim3(256), s, a);
     };
     if (half <= 8) return go(std::integral_constant<int, 8>());
     if (half <= 16) return go(std::integral_constant<int, 16>());
@@ -567,7 +685,7 @@ hipError_t launch_logp(const LogpArgs<T>& a, int units, hipStream_t s) {
   //   Few rows wait for one another's steps, so more threads: 1 x 32768 bf16, 1024 and 4 7.5, 512 and 8
   //   8.2; 20 x 50000 f32 by 1024 15, by 512 17.
 #define NF_ROW(TH, NV) \
-  return launch_k(logp_row_kernel<T, TH, NV, GRAD>, dim3((unsigned)a.rows), dim3(TH), 0, s, a)
+  return op_launch(logp_row_kernel<T, TH, NV, GRAD>, dim3((unsigned)a.rows), dim3(TH), s, a)
   const bool few = a.rows <= units;
   if (vecs <= 64) NF_ROW(64, 1);
   if (vecs <= 256) NF_ROW(64, 4);
@@ -616,6 +734,15 @@ nf_status check_gradient(const void* x, int64_t ld, const void* dx, int64_t ld_d
   return NF_OK;
 }
 
+// The workspace may be left out: rows then stay whole.
+nf_status check_logp_work(const void* work, int64_t have, const LogpPlan& p) {
+  if (!work || !p.slices) return NF_OK;
+  if (!op_aligned(work, 16)) return op_fail(NF_EINVAL, "the workspace is not aligned to 16 bytes");
+  if (have < p.bytes)
+    return op_fail(NF_ESHAPE, "the workspace has %lld bytes, %lld are needed", (long long)have, (long long)p.bytes);
+  return NF_OK;
+}
+
 }  // namespace
 
 int op_compute_units() {
@@ -643,9 +770,18 @@ using namespace nf;
 
 extern "C" {
 
+int64_t nf_logprobs_work(int32_t dtype, int64_t rows, int64_t classes, int32_t n_top, int32_t gradient) {
+  op_begin();
+  if (!op_float_type(dtype) || rows < 0 || classes < 1 || n_top < 0 || n_top > NF_TOP_MAX || classes > (1 << 30)) {
+    op_fail(NF_EINVAL, "sizes or type that the call would refuse");
+    return -1;
+  }
+  return logp_plan(op_size(dtype), rows, classes, gradient ? 0 : n_top, gradient != 0).bytes;
+}
+
 nf_status nf_logprobs(const void* d_logits, int32_t dtype, int64_t rows, int64_t classes, int64_t ld, float scale,
                       const int64_t* d_targets, int32_t n_top, float* d_logp, float* d_entropy, float* d_stat,
-                      int32_t* d_top_ids, float* d_top_logp, void* stream) {
+                      int32_t* d_top_ids, float* d_top_logp, void* d_work, int64_t work_bytes, void* stream) {
   op_begin();
   const nf_status st = check_logits(d_logits, dtype, rows, classes, ld, scale);
   if (st != NF_OK) return st;
@@ -653,6 +789,9 @@ nf_status nf_logprobs(const void* d_logits, int32_t dtype, int64_t rows, int64_t
   if (n_top > classes) return op_fail(NF_ESHAPE, "more alternatives than classes");
   if (n_top > 0 && !d_top_ids && !d_top_logp) return op_fail(NF_EINVAL, "alternatives without a place for them");
   if (rows == 0) return NF_OK;
+  const LogpPlan plan = logp_plan(op_size(dtype), rows, classes, n_top, false);
+  const nf_status ws = check_logp_work(d_work, work_bytes, plan);
+  if (ws != NF_OK) return ws;
   const int units = op_compute_units();
   if (units <= 0) return op_fail(NF_EDEVICE, "no usable HIP device");
   return with_type(dtype, [&](auto e) {
@@ -670,20 +809,26 @@ nf_status nf_logprobs(const void* d_logits, int32_t dtype, int64_t rows, int64_t
     a.stat = d_stat;
     a.top_ids = d_top_ids;
     a.top_logp = d_top_logp;
-    return op_result(launch_logp<T, false>(a, units, static_cast<hipStream_t>(stream)), "log probabilities");
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return op_result(plan.slices && d_work ? launch_parts<T>(a, plan, static_cast<char*>(d_work), s)
+                                           : launch_logp<T, false>(a, units, s),
+                     "log probabilities");
   });
 }
 
 nf_status nf_logprobs_train(const void* d_logits, int32_t dtype, int64_t rows, int64_t classes, int64_t ld,
                             float scale, const int64_t* d_targets, const float* d_g_logp, const float* d_g_entropy,
                             float* d_logp, float* d_entropy, float* d_stat, void* d_dlogits, int64_t ld_d,
-                            void* stream) {
+                            void* d_work, int64_t work_bytes, void* stream) {
   op_begin();
   nf_status st = check_logits(d_logits, dtype, rows, classes, ld, scale);
   if (st != NF_OK) return st;
   if (rows == 0) return NF_OK;
   if (d_g_logp && !d_targets) return op_fail(NF_EINVAL, "weights of log probabilities without targets");
   st = check_gradient(d_logits, ld, d_dlogits, ld_d, dtype, rows, classes);
+  if (st != NF_OK) return st;
+  const LogpPlan plan = logp_plan(op_size(dtype), rows, classes, 0, true);
+  st = check_logp_work(d_work, work_bytes, plan);
   if (st != NF_OK) return st;
   const int units = op_compute_units();
   if (units <= 0) return op_fail(NF_EDEVICE, "no usable HIP device");
@@ -703,7 +848,28 @@ nf_status nf_logprobs_train(const void* d_logits, int32_t dtype, int64_t rows, i
     a.entropy = d_entropy;
     a.stat = d_stat;
     a.dx = static_cast<T*>(d_dlogits);
-    return op_result(launch_logp<T, true>(a, units, static_cast<hipStream_t>(stream)), "log probabilities and gradient");
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (!plan.slices || !d_work) return op_result(launch_logp<T, true>(a, units, s), "log probabilities and gradient");
+    // the slices' sums, and the gradient from what they come to
+    char* const work = static_cast<char*>(d_work);
+    if (!a.stat) a.stat = reinterpret_cast<float*>(work + plan.stat);
+    if (!a.entropy) a.entropy = reinterpret_cast<float*>(work + plan.entropy);
+    hipError_t he = launch_parts<T>(a, plan, work, s);
+    if (he != hipSuccess) return op_result(he, "log probabilities");
+    GradArgs<T> g{};
+    g.x = a.x;
+    g.dx = a.dx;
+    g.ld = ld;
+    g.ld_dx = ld_d;
+    g.rows = rows;
+    g.classes = (int)classes;
+    g.scale = scale;
+    g.target = d_targets;
+    g.stat = a.stat;
+    g.entropy = a.entropy;
+    g.g = d_g_logp;
+    g.h = d_g_entropy;
+    return op_result(launch_grad<T>(g, s), "gradient of log probabilities");
   });
 }
 
@@ -731,19 +897,14 @@ nf_status nf_logprobs_grad(const void* d_logits, int32_t dtype, int64_t rows, in
     a.ld_dx = ld_d;
     a.rows = rows;
     a.classes = (int)classes;
-    constexpr int64_t per = 256 * Vec16<T>::N * GRAD_VECS;
-    a.per_row = (int)((classes + per - 1) / per);
-    a.blocks = rows * a.per_row;
-    if (a.blocks > 0x7fffffff) return op_fail(NF_ESHAPE, "too many logits for one call");
     a.scale = scale;
     a.target = d_targets;
     a.stat = d_stat;
     a.entropy = d_entropy;
     a.g = d_g_logp;
     a.h = d_g_entropy;
-    return op_result(launch_k(logp_grad_kernel<T>, dim3((unsigned)a.blocks), dim3(256), 0,
-                              static_cast<hipStream_t>(stream), a),
-                     "gradient of log probabilities");
+    if (rows * ((classes + 255) / 256) > 0x7fffffff) return op_fail(NF_ESHAPE, "too many logits for one call");
+    return op_result(launch_grad<T>(a, static_cast<hipStream_t>(stream)), "gradient of log probabilities");
   });
 }
 

@@ -495,8 +495,8 @@ hipError_t launch_tile(MmArgs a, int64_t count, hipStream_t s) {
   a.mt = (rows + BM - 1) / BM;
   a.nt = (cols + BM - 1) / BM;
   a.total = SQUARE ? a.mt * (a.mt + 1) / 2 : a.mt * a.nt;
-  return launch_k(orth_mm_kernel<KIND, PROD, BM, BM, WM, WN, NS, G, OCC>, dim3(mm_grid(a.total), (unsigned)count),
-                  dim3((BM / WM) * (BM / WN) * G * 64), 0, s, a);
+  return op_launch(orth_mm_kernel<KIND, PROD, BM, BM, WM, WN, NS, G, OCC>, dim3(mm_grid(a.total), (unsigned)count),
+                  dim3((BM / WM) * (BM / WN) * G * 64), s, a);
 }
 
 template <int KIND, int PROD>
@@ -581,7 +581,7 @@ hipError_t orth_run(const OrthCall& c, int units, hipStream_t s) {
   // 2048 values a workgroup and more, and enough workgroups for the card
   const int64_t want = (c.rows * c.cols + 2047) / 2048;
   const int blocks = (int)(want < SUM_BLOCKS ? want : SUM_BLOCKS);
-  hipError_t e = launch_k(orth_sum_kernel<T>, dim3((unsigned)blocks, (unsigned)c.count), dim3(256), 0, s, u);
+  hipError_t e = op_launch(orth_sum_kernel<T>, dim3((unsigned)blocks, (unsigned)c.count), dim3(256), s, u);
   if (e != hipSuccess) return e;
   FillArgs<T> f{};
   f.g = u.g;
@@ -592,8 +592,8 @@ hipError_t orth_run(const OrthCall& c, int units, hipStream_t s) {
   f.blocks = blocks;
   f.work = work;
   f.p = p;
-  e = launch_k(orth_fill_kernel<T, KIND>, dim3((unsigned)((p.n + 63) / 64), (unsigned)((p.m + 63) / 64), (unsigned)c.count),
-               dim3(256), 0, s, f);
+  e = op_launch(orth_fill_kernel<T, KIND>, dim3((unsigned)((p.n + 63) / 64), (unsigned)((p.m + 63) / 64), (unsigned)c.count),
+               dim3(256), s, f);
   if (e != hipSuccess) return e;
   MmArgs a{};
   a.p = p;

@@ -110,6 +110,14 @@ inline nf_status op_result(hipError_t e, const char* what) {
   return op_fail(NF_EDEVICE, "%s: %s", what, hipGetErrorString(e));
 }
 
+// Launches a kernel of an operator (a plain launch: nothing times these one by one).
+template <typename... P>
+inline hipError_t op_launch(void (*kernel)(P...), dim3 grid, dim3 block, hipStream_t s,
+                            const typename same_type<P>::type&... args) {
+  void* argv[] = {const_cast<void*>(static_cast<const void*>(&args))..., nullptr};
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, argv, 0, s);
+}
+
 // Compute units of the current device, or 0 where there is none (asked once
 // for each device).
 int op_compute_units();

@@ -32,7 +32,7 @@ __device__ __forceinline__ float direction(float g, float m, float momentum, boo
 }
 
 constexpr int ORTH_SMALL = 64;
-constexpr int SMALL_COLS = 128;         // columns that a workgroup of the Gram matrix holds at a time
+constexpr int SMALL_COLS = 64;         // columns that a workgroup of the Gram matrix holds at a time
 constexpr int SMALL_PARTS = 16;         // at most; partial Gram matrices
 constexpr int SMALL_OUT = 64;           // columns that a workgroup of the result has
 
@@ -192,62 +192,93 @@ __global__ void __launch_bounds__(64 * CHAIN_WAVES) small_chain_kernel(char* wor
     __syncthreads();
   };
   each([&](int, int, int o) { lds[A + o] *= inv; });
-  // C = f(X Y, i, j, place) for matrices that commute and are symmetric: rows by rows.
-  // A block's operands are read before its first instruction, which would wait for
-  // each pair otherwise.
-  auto product = [&](int C, int X, int Y, auto&& f) {
+  // Products of matrices that commute and are symmetric: rows by rows, half the
+  // blocks.  A block's operands are read before its first instruction, which would
+  // wait for each pair otherwise; r[v] is element (4 v + lane / 16, lane % 16) of block k.
+  auto form = [&](int X, int Y, int k, double (&r)[4]) {
+    const double* const px = lds + X + (16 * small_row(k) + (lane & 15)) * S::PITCH + (lane >> 4);
+    const double* const py = lds + Y + (16 * small_col(k) + (lane & 15)) * S::PITCH + (lane >> 4);
+    double x[S::M / 4], y[S::M / 4];
+#pragma unroll
+    for (int s = 0; s < S::M / 4; ++s) {
+      x[s] = px[4 * s];
+      y[s] = py[4 * s];
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    // two sums, so that the instructions do not all wait for one another
+    doublex4 c0 = {}, c1 = {};
+#pragma unroll
+    for (int s = 0; s < S::M / 4; s += 2) {
+      c0 = __builtin_amdgcn_mfma_f64_16x16x4f64(x[s], y[s], c0, 0, 0, 0);
+      c1 = __builtin_amdgcn_mfma_f64_16x16x4f64(x[s + 1], y[s + 1], c1, 0, 0, 0);
+    }
+#pragma unroll
+    for (int v = 0; v < 4; ++v) r[v] = c0[v] + c1[v];
+  };
+  auto place = [&](int k, int v, int& i, int& j) {
+    i = 16 * small_row(k) + 4 * v + (lane >> 4);
+    j = 16 * small_col(k) + (lane & 15);
+    return i * S::PITCH + j;
+  };
+  auto keep = [&](int C, int k, const double (&r)[4]) {
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      int i, j;
+      lds[C + place(k, v, i, j)] = r[v];
+      if (small_row(k) != small_col(k)) lds[C + j * S::PITCH + i] = r[v];
+    }
+  };
+  constexpr int MINE = (S::BLOCKS + CHAIN_WAVES - 1) / CHAIN_WAVES;     // of P's blocks, at most
+  for (int step = 0; step < steps; ++step) {
+    const bool last = step + 1 == steps;
+    // Q = a + b A + c A^2
     for (int k = wave; k < S::BLOCKS; k += CHAIN_WAVES) {
-      const int a = small_row(k), b = small_col(k);
-      const double* const px = lds + X + (16 * a + (lane & 15)) * S::PITCH + (lane >> 4);
-      const double* const py = lds + Y + (16 * b + (lane & 15)) * S::PITCH + (lane >> 4);
-      double x[S::M / 4], y[S::M / 4];
-#pragma unroll
-      for (int s = 0; s < S::M / 4; ++s) {
-        x[s] = px[4 * s];
-        y[s] = py[4 * s];
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      // two sums, so that the instructions do not all wait for one another
-      doublex4 c0 = {}, c1 = {};
-#pragma unroll
-      for (int s = 0; s < S::M / 4; s += 2) {
-        c0 = __builtin_amdgcn_mfma_f64_16x16x4f64(x[s], y[s], c0, 0, 0, 0);
-        c1 = __builtin_amdgcn_mfma_f64_16x16x4f64(x[s + 1], y[s + 1], c1, 0, 0, 0);
-      }
       double r[4];
+      form(A, A, k, r);
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        const int i = 16 * a + 4 * v + (lane >> 4), j = 16 * b + (lane & 15);
-        r[v] = f(c0[v] + c1[v], i, j, i * S::PITCH + j);
+        int i, j;
+        const int o = place(k, v, i, j);
+        r[v] = (double)qc * r[v] + (double)qb * lds[A + o] + (i == j ? (double)qa : 0.0);
       }
-#pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const int i = 16 * a + 4 * v + (lane >> 4), j = 16 * b + (lane & 15);
-        lds[C + i * S::PITCH + j] = r[v];
-        if (a != b) lds[C + j * S::PITCH + i] = r[v];
-      }
+      keep(Q, k, r);
     }
     __syncthreads();
-  };
-  auto plain = [](double x, int, int, int) { return x; };
-  for (int k = 0; k < steps; ++k) {
-    product(Q, A, A, [&](double x, int i, int j, int o) {
-      return (double)qc * x + (double)qb * lds[A + o] + (i == j ? (double)qa : 0.0);
-    });
-    if (k + 1 < steps) {
-      product(R, A, Q, plain);
-      product(A, R, Q, plain);
+    // R = A Q and, from the second step on, P = Q P, whose old values are read until all are formed
+    double mine[MINE][4];
+#pragma unroll
+    for (int n = 0; n < MINE; ++n) {
+      const int k = CHAIN_WAVES - 1 - wave + n * CHAIN_WAVES;           // (the waves that R leaves idle first)
+      if (step > 0 && k < S::BLOCKS) form(Q, P, k, mine[n]);
     }
-    int spare = Q;
-    if (k > 0) {
-      product(R, Q, P, plain);
-      spare = R;
+    if (!last)
+      for (int k = wave; k < S::BLOCKS; k += CHAIN_WAVES) {
+        double r[4];
+        form(A, Q, k, r);
+        keep(R, k, r);
+      }
+    __syncthreads();
+    if (step > 0) {
+#pragma unroll
+      for (int n = 0; n < MINE; ++n) {
+        const int k = CHAIN_WAVES - 1 - wave + n * CHAIN_WAVES;
+        if (k < S::BLOCKS) keep(P, k, mine[n]);
+      }
     }
-    // the product so far is P; what held the old one is free
-    const int old = P;
-    P = spare;
-    if (spare == Q) Q = old;
-    else R = old;
+    // A = R Q
+    if (!last)
+      for (int k = wave; k < S::BLOCKS; k += CHAIN_WAVES) {
+        double r[4];
+        form(R, Q, k, r);
+        keep(A, k, r);
+      }
+    if (step == 0) {                     // P = Q: its place takes the next step's Q
+      __syncthreads();
+      const int old = P;
+      P = Q;
+      Q = old;
+    }
+    __syncthreads();
   }
   const double size = sqrt(inv);
   double* const out = reinterpret_cast<double*>(w + p.p);
@@ -314,11 +345,11 @@ __global__ void __launch_bounds__(256) small_apply_kernel(const SmallArgs<T> a) 
 
 template <class T, int MB>
 hipError_t launch_small(const SmallArgs<T>& a, int64_t count, float qa, float qb, float qc, int steps, hipStream_t s) {
-  hipError_t e = launch_k(small_gram_kernel<T, MB>, dim3((unsigned)a.p.parts, (unsigned)count), dim3(256), 0, s, a);
+  hipError_t e = op_launch(small_gram_kernel<T, MB>, dim3((unsigned)a.p.parts, (unsigned)count), dim3(256), s, a);
   if (e != hipSuccess) return e;
-  e = launch_k(small_chain_kernel<MB>, dim3((unsigned)count), dim3(64 * CHAIN_WAVES), 0, s, a.work, a.p, qa, qb, qc, steps);
+  e = op_launch(small_chain_kernel<MB>, dim3((unsigned)count), dim3(64 * CHAIN_WAVES), s, a.work, a.p, qa, qb, qc, steps);
   if (e != hipSuccess) return e;
-  return launch_k(small_apply_kernel<T, MB>, dim3((unsigned)((a.p.n + SMALL_OUT - 1) / SMALL_OUT), (unsigned)count), dim3(256), 0, s, a);
+  return op_launch(small_apply_kernel<T, MB>, dim3((unsigned)((a.p.n + SMALL_OUT - 1) / SMALL_OUT), (unsigned)count), dim3(256), s, a);
 }
 
 }  // namespace nf

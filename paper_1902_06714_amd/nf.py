@@ -122,9 +122,11 @@ _sig = {
 }
 _p, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
 _sig.update({
-    "nf_logprobs": (ctypes.c_int, [_p, _i32, _i64, _i64, _i64, _f32, _p, _i32, _p, _p, _p, _p, _p, _p]),
+    "nf_logprobs_work": (_i64, [_i32, _i64, _i64, _i32, _i32]),
+    "nf_logprobs": (ctypes.c_int, [_p, _i32, _i64, _i64, _i64, _f32, _p, _i32, _p, _p, _p, _p, _p, _p,
+                                   _i64, _p]),
     "nf_logprobs_train": (ctypes.c_int, [_p, _i32, _i64, _i64, _i64, _f32, _p, _p, _p, _p, _p, _p,
-                                         _p, _i64, _p]),
+                                         _p, _i64, _p, _i64, _p]),
     "nf_logprobs_grad": (ctypes.c_int, [_p, _i32, _i64, _i64, _i64, _f32, _p, _p, _p, _p, _p, _p,
                                         _i64, _p]),
     "nf_orthogonalize_work": (_i64, [_i32, _i64, _i64, _i64]),
@@ -488,8 +490,24 @@ def _workspace(work, need: int, stream, name: str):
     return work.data_ptr(), work.numel() * work.element_size(), work
 
 
+def nf_logprobs_work(dtype: int, rows: int, classes: int, n_top: int = 0, gradient: bool = False) -> int:
+    """Bytes of a workspace that is of use; raises for sizes that would be refused."""
+    n = _lib.nf_logprobs_work(dtype, rows, classes, n_top, int(gradient))
+    if n < 0:
+        raise NfError(NF_EINVAL, "nf_logprobs_work")
+    return n
+
+
+def _few_rows(code: int, rows: int, cols: int, n_top: int, gradient: int, work, stream):
+    """The workspace of few long rows; none for others (many or short ones need none)."""
+    if work is None and (rows > 64 or cols < 16384):
+        return None, 0, None
+    need = _lib.nf_logprobs_work(code, rows, cols, n_top, gradient)
+    return _workspace(work, need, stream, "nf_logprobs_work") if need > 0 else (None, 0, None)
+
+
 def nf_logprobs(logits, targets=None, logp=None, entropy=None, stat=None, top_ids=None, top_logp=None,
-                scale: float = 1.0, stream=None) -> None:
+                scale: float = 1.0, work=None, stream=None) -> None:
     """logits [rows][classes], targets [rows] int64; logp, entropy [rows], stat
     [rows][2], top_ids (int32) and top_logp [rows][n_top] receive what they name."""
     code = _elem(logits, "logits")
@@ -497,10 +515,11 @@ def nf_logprobs(logits, targets=None, logp=None, entropy=None, stat=None, top_id
     top = top_ids if top_ids is not None else top_logp
     n_top = 0 if top is None else top.shape[-1]
     row = (rows,)
+    w, n, keep = _few_rows(code, rows, cols, n_top, 0, work, stream)
     st = _lib.nf_logprobs(x, code, rows, cols, ld, scale, _vector(targets, "targets", _i64_t, row), n_top,
                           _vector(logp, "logp", _f32_t, row), _vector(entropy, "entropy", _f32_t, row),
                           _vector(stat, "stat", _f32_t, (rows, 2)), _vector(top_ids, "top_ids", _i32_t, (rows, n_top)),
-                          _vector(top_logp, "top_logp", _f32_t, (rows, n_top)), _queue(stream))
+                          _vector(top_logp, "top_logp", _f32_t, (rows, n_top)), w, n, _queue(stream))
     if st:
         raise NfError(st, "nf_logprobs")
 
@@ -513,17 +532,18 @@ def _like(t, of, code: int, name: str):
 
 
 def nf_logprobs_train(logits, targets, g_logp, g_entropy, dlogits, logp=None, entropy=None, stat=None,
-                      scale: float = 1.0, stream=None) -> None:
+                      scale: float = 1.0, work=None, stream=None) -> None:
     """nf_logprobs with the gradient of sum(g_logp logp + g_entropy entropy) in
     dlogits [rows][classes], which may be the logits."""
     code = _elem(logits, "logits")
     x, rows, cols, ld = _matrix(logits, "logits")
     dx, ldd = _like(dlogits, logits, code, "dlogits")
     row = (rows,)
+    w, n, keep = _few_rows(code, rows, cols, 0, 1, work, stream)
     st = _lib.nf_logprobs_train(x, code, rows, cols, ld, scale, _vector(targets, "targets", _i64_t, row),
                                 _vector(g_logp, "g_logp", _f32_t, row), _vector(g_entropy, "g_entropy", _f32_t, row),
                                 _vector(logp, "logp", _f32_t, row), _vector(entropy, "entropy", _f32_t, row),
-                                _vector(stat, "stat", _f32_t, (rows, 2)), dx, ldd, _queue(stream))
+                                _vector(stat, "stat", _f32_t, (rows, 2)), dx, ldd, w, n, _queue(stream))
     if st:
         raise NfError(st, "nf_logprobs_train")
 

@@ -200,6 +200,48 @@ def test_logprobs_long_rows(dtype, classes, kind):
     _check_logprobs(dtype, 5, classes, kind, 9, 1, classes % 2, 1.25, grad=kind in ("plain", "masked", "bad"))
 
 
+# more rows than compute units, or too many to be cut: other numbers of threads
+@pytest.mark.parametrize("rows,dtype,classes,kind", [
+    (300, "bf16", 2500, "plain"), (300, "f32", 3000, "masked"), (300, "bf16", 5003, "bad"), (300, "f16", 12000, "plain"),
+    (300, "bf16", 32767, "masked"), (300, "f32", 16500, "plain"), (70, "f32", 66001, "plain"), (70, "bf16", 30000, "ties"),
+    (300, "f32", 4097, "ties")])
+def test_logprobs_many_rows(rows, dtype, classes, kind):
+    _check_logprobs(dtype, rows, classes, kind, 0 if classes > 20000 and kind != "ties" else 6, 2, 1, 1.0)
+
+
+# few rows that are cut, the last slice shorter than the alternatives, and the same rows whole
+@pytest.mark.parametrize("rows,dtype,classes,n_top", [
+    (1, "bf16", 49152, 1), (1, "bf16", 131072, 64), (2, "f32", 24581, 20), (64, "bf16", 65600, 3), (33, "f16", 131071, 7),
+    (1, "f32", 300001, 64), (17, "f32", 65536, 5)])
+@pytest.mark.parametrize("kind", ["plain", "ties", "bad"])
+def test_logprobs_few_long_rows(rows, dtype, classes, n_top, kind):
+    torch, nf = torch_cuda(), _nf()
+    if rows * classes <= 1 << 20:
+        _check_logprobs(dtype, rows, classes, kind, n_top, 1, 1, 0.7, grad=kind != "ties")
+    rng = np.random.default_rng(classes)
+    note(f"few long rows {dtype} {rows}x{classes} {kind} top={n_top}")
+    x = _dev(_logits(rng, rows, classes, kind), _dt(dtype))
+    t = _dev(rng.integers(0, classes, rows))
+    code = {"f32": nf.NF_F32, "bf16": nf.NF_BF16, "f16": nf.NF_F16}[dtype]
+    assert nf.nf_logprobs_work(code, rows, classes, n_top) > 0
+    outs = []
+    for whole in (False, True):
+        logp, ent, stat = (_empty(s, torch.float32) for s in ((rows,), (rows,), (rows, 2)))
+        ids, alt = _empty((rows, n_top), torch.int32), _empty((rows, n_top), torch.float32)
+        if whole:
+            st = nf.raw().nf_logprobs(x.data_ptr(), code, rows, classes, classes, 1.0, t.data_ptr(), n_top, logp.data_ptr(),
+                                      ent.data_ptr(), stat.data_ptr(), ids.data_ptr(), alt.data_ptr(), None, 0,
+                                      torch.cuda.current_stream().cuda_stream)
+            assert st == nf.NF_OK
+        else:
+            nf.nf_logprobs(x, t, logp, ent, stat, ids, alt)
+        torch.cuda.synchronize()
+        outs.append((logp, ent, stat[:, 1], alt, ids))
+    assert torch.equal(outs[0][4], outs[1][4])
+    for a, b in zip(outs[0][:4], outs[1][:4]):
+        _same(_np(a), _np(b), 3e-5, "cut and whole")
+
+
 @pytest.mark.parametrize("rows", [1, 2, 63, 64, 65, 1001])
 @pytest.mark.parametrize("classes", [3, 10, 30, 100])
 def test_logprobs_many_short_rows(rows, classes):
@@ -255,7 +297,8 @@ def _rel(got, want):
 
 
 SHAPES = [(1, 1), (1, 7), (7, 1), (2, 2), (3, 200), (30, 784), (64, 64), (65, 63), (100, 1), (129, 257), (200, 96),
-          (300, 300), (517, 259), (259, 1001)]
+          (300, 300), (517, 259), (259, 1001), (16, 65), (17, 130), (33, 32), (32, 4100), (48, 49), (49, 1200), (2100, 64),
+          (65, 65), (65, 3000), (96, 97)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -436,7 +479,8 @@ def _linear_case(rows, inputs, outputs, x_dtype, y_dtype, act, bias, pad=0, garb
 
 
 @pytest.mark.parametrize("rows,inputs,outputs", [
-    (1, 1, 1), (1, 16, 10), (1, 784, 30), (1, 4097, 515), (2, 1001, 17), (5, 17, 259), (16, 784, 1024), (17, 100, 64),
+    (1, 1, 1), (1, 16, 10), (1, 784, 30), (1, 4097, 515), (2, 1001, 17), (3, 4096, 100), (4, 16320, 40), (4, 20000, 33),
+    (5, 17, 259), (6, 784, 90), (15, 4100, 48), (16, 784, 1024), (17, 100, 64),
     (31, 2049, 33), (33, 1001, 517), (64, 64, 64), (65, 130, 100), (200, 784, 300), (257, 513, 129),
     (1000, 129, 77), (3, 30000, 20), (70, 9000, 70)])
 @pytest.mark.parametrize("x_dtype,y_dtype", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f16"), ("bf16", "f32")])

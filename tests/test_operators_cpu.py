@@ -75,11 +75,11 @@ def test_every_operator_is_declared_and_exported():
     with open(nf.HEADER) as f:
         text = re.sub(r"/\*.*?\*/", "", f.read(), flags=re.S)
     names = set(re.findall(r"\b(nf_\w+)\s*\(", text))
-    want = {"nf_logprobs", "nf_logprobs_train", "nf_logprobs_grad", "nf_orthogonalize_work", "nf_orthogonalize",
+    want = {"nf_logprobs_work", "nf_logprobs", "nf_logprobs_train", "nf_logprobs_grad", "nf_orthogonalize_work", "nf_orthogonalize",
             "nf_muon_step", "nf_quantize_rows", "nf_linear_i8", "nf_linear_i8_work", "nf_linear_i8_dynamic"}
     assert want <= names
     for n in want:
-        assert hasattr(nf.raw(), n) and callable(getattr(nf, n, None)) or n == "nf_linear_i8_work"
+        assert hasattr(nf.raw(), n) and callable(getattr(nf, n))
 
 
 # Addresses that no refused call may touch: the arguments are checked first.
@@ -97,9 +97,9 @@ def _call(name, base, change):
 
 
 LOGP = dict(x=P, dtype=nf.NF_BF16, rows=4, classes=10, ld=10, scale=1.0, t=P, n_top=2, logp=P, ent=P, stat=P, ids=P,
-            alt=P, stream=None)
+            alt=P, work=None, bytes=0, stream=None)
 TRAIN = dict(x=P, dtype=nf.NF_F32, rows=4, classes=10, ld=10, scale=1.0, t=P, g=P, h=P, logp=P, ent=P, stat=P,
-             dx=2 * P, ldd=10, stream=None)
+             dx=2 * P, ldd=10, work=None, bytes=0, stream=None)
 GRAD = dict(x=P, dtype=nf.NF_F32, rows=4, classes=10, ld=10, scale=1.0, t=P, stat=P, ent=P, g=P, h=P, dx=2 * P, ldd=10,
             stream=None)
 ORTH = dict(x=P, dtype=nf.NF_F32, count=2, rows=6, cols=8, ld=8, stride=48, out=2 * P, ldo=8, so=48, work=4 * P,
@@ -123,6 +123,9 @@ DYN = dict(x=P, xd=nf.NF_F32, ldx=17, wq=2 * P, ldw=32, ws=P, bias=P, act=1, row
     ("nf_logprobs", LOGP, {"scale": INF}, E), ("nf_logprobs", LOGP, {"scale": NAN}, E),
     ("nf_logprobs", LOGP, {"n_top": -1}, E), ("nf_logprobs", LOGP, {"n_top": 65, "classes": 100, "ld": 100}, E),
     ("nf_logprobs", LOGP, {"n_top": 11}, S), ("nf_logprobs", LOGP, {"ids": None, "alt": None}, E),
+    ("nf_logprobs", LOGP, {"classes": 131072, "ld": 131072, "work": P, "bytes": 10}, S),
+    ("nf_logprobs", LOGP, {"classes": 131072, "ld": 131072, "work": P + 8, "bytes": BIG}, E),
+    ("nf_logprobs_train", TRAIN, {"classes": 131072, "ld": 131072, "ldd": 131072, "dx": 99 * P, "work": P, "bytes": 10}, S),
     ("nf_logprobs_train", TRAIN, {"dx": None}, E), ("nf_logprobs_train", TRAIN, {"ldd": 9}, S),
     ("nf_logprobs_train", TRAIN, {"dx": P + 8}, E), ("nf_logprobs_train", TRAIN, {"dx": P, "ldd": 12}, E),
     ("nf_logprobs_train", TRAIN, {"dx": 2 * P + 2}, E), ("nf_logprobs_train", TRAIN, {"t": None}, E),
@@ -180,6 +183,9 @@ def test_workspace_sizes():
     assert lib.nf_orthogonalize_work(nf.NF_F16, 1, 4, 4) == -1 and nf.nf_last_error() != ""
     assert lib.nf_orthogonalize_work(nf.NF_F32, 1, 0, 4) == -1
     assert lib.nf_orthogonalize_work(nf.NF_F32, 0, 4, 4) == 0
+    assert lib.nf_logprobs_work(nf.NF_F64, 1, 10, 0, 0) == -1 and lib.nf_logprobs_work(nf.NF_F32, 1, 10, 65, 0) == -1
+    assert lib.nf_logprobs_work(nf.NF_F32, 1000, 131072, 5, 0) == 0 and lib.nf_logprobs_work(nf.NF_F32, 1, 1000, 5, 0) == 0
+    assert lib.nf_logprobs_work(nf.NF_F32, 1, 131072, 5, 0) > 0 and lib.nf_logprobs_work(nf.NF_F32, 0, 131072, 5, 1) == 0
     one = lib.nf_orthogonalize_work(nf.NF_F32, 1, 30, 784)
     assert one > 0 and lib.nf_orthogonalize_work(nf.NF_F32, 5, 30, 784) == 5 * one
     assert lib.nf_orthogonalize_work(nf.NF_F32, 1, 784, 30) == one
