@@ -15,10 +15,12 @@ a second one.  The Python binding imports torch before loading the library.
 from __future__ import annotations
 
 import concurrent.futures
+import importlib.util
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -31,6 +33,8 @@ SOURCES = ["nf_api.hip", "nf_kernels.hip", "nf_narrow.hip", "nf_narrow64.hip", "
 # the operators on the caller's own arrays, apart from the net's kernels
 OPS = os.path.join(HERE, "csrc_ops")
 OPS_SOURCES = ["nf_logprobs.hip", "nf_orth.hip", "nf_linear_i8.hip"]
+# their calls with torch tensors, a Python module of host code
+BIND = os.path.join(HERE, "_nfbind.so")
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",
@@ -50,6 +54,12 @@ def hipcc() -> str:
     raise RuntimeError("hipcc not found (ROCm is required to build the library)")
 
 
+def torch_dir():
+    """Where torch is installed (found without importing it); None where it is not."""
+    spec = importlib.util.find_spec("torch")
+    return os.path.dirname(spec.origin) if spec and spec.origin else None
+
+
 def _run(cmd, verbose):
     if verbose:
         print(" ".join(cmd), flush=True)
@@ -66,6 +76,14 @@ def build(verbose: bool = False) -> str:
     objs = [os.path.join(objdir, os.path.splitext(os.path.basename(p))[0] + ".o") for p in paths]
     cmds = [[hipcc(), *HIPCC_FLAGS, "-c", "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-I", OPS,
              path, "-o", obj] for path, obj in zip(paths, objs)]
+    torch = torch_dir()
+    bind = os.path.join(objdir, "nf_bind.o")
+    if torch:
+        cmds.append(["g++", "-O2", "-std=c++17", "-fPIC", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=1",
+                     "-I", sysconfig.get_paths()["include"], "-I", os.path.join(ROOT, "include"),
+                     "-isystem", os.path.join(torch, "include"),
+                     "-isystem", os.path.join(torch, "include", "torch", "csrc", "api", "include"),
+                     "-c", os.path.join(OPS, "nf_bind.cpp"), "-o", bind])
     # one compiler process per source, at most as many as the CPUs this
     # process may use
     workers = max(1, min(len(cmds), len(os.sched_getaffinity(0)), 8))
@@ -76,6 +94,13 @@ def build(verbose: bool = False) -> str:
     tmp = LIB + ".tmp"
     _run([hipcc(), "-shared", "-fPIC", *objs, "-o", tmp, f"-Wl,-rpath,{rocm_lib}"], verbose)
     os.replace(tmp, LIB)
+    if torch is None:                       # no tensors to call the operators with
+        return LIB
+    tmp = BIND + ".tmp"
+    _run(["g++", "-shared", "-fPIC", bind, "-o", tmp, "-L", HERE, "-l:" + os.path.basename(LIB),
+          "-L", os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath,$ORIGIN",
+          "-Wl,-rpath," + os.path.join(torch, "lib")], verbose)
+    os.replace(tmp, BIND)
     return LIB
 
 

@@ -1,5 +1,5 @@
-"""ctypes binding of include/nf.h: the same entry points, argument marshalling
-only.  Every step of the computation runs in the HIP library; there is no
+"""Binding of include/nf.h, by ctypes and for the operators on tensors by a small
+module of compiled code: the same entry points, argument marshalling only.  Every step of the computation runs in the HIP library; there is no
 other implementation behind these functions.  Importing this module fails
 loudly when the library has not been built.
 
@@ -418,76 +418,43 @@ def nf_calib_spin(us: float, stream=None) -> None:
 
 # -- operators on the caller's own tensors ------------------------------------
 # Matrices are 2-D (stacks 3-D) GPU tensors whose rows are contiguous; vectors
-# are contiguous.  Outputs are the caller's tensors; None leaves one out.
+# are contiguous.  Outputs are the caller's tensors; None leaves one out.  The
+# tensors are checked and taken apart in _nfbind (csrc_ops/nf_bind.cpp).
 NF_TOP_MAX, NF_ORTH_MAX, NF_ORTH_MAX_LD, NF_ORTH_STEPS = 64, 65536, 1 << 20, 5
 NF_LINEAR_I8_MAX, NF_NO_ACT = 131071, -1
+
+
 try:
-    _f32_t, _i32_t, _i64_t, _i8_t = torch.float32, torch.int32, torch.int64, torch.int8
-    _elems = {torch.float32: NF_F32, torch.bfloat16: NF_BF16, torch.float16: NF_F16}
-    _device = torch._C._cuda_getDevice
-    _raw_stream = torch._C._cuda_getCurrentRawStream
-except (NameError, AttributeError):     # no torch, or one without a GPU: no tensor passes the checks
-    _f32_t = _i32_t = _i64_t = _i8_t = None
-    _elems = {}
+    import torch
+except ImportError:
+    pass
+else:
+    if not os.path.exists(os.path.join(_HERE, "_nfbind.so")):
+        raise ImportError("_nfbind.so is missing: build the library first "
+                          "(python -m paper_1902_06714_amd.build, or __graft_entry__.build())")
+    from . import _nfbind
 
 
-def _tensor(t, name: str):
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a torch tensor on the GPU")
-    return t
+def _on(stream, work, need, *args):
+    """(stream for _nfbind, workspace): the current stream's workspace comes from there;
+    on another stream it is kept by torch's allocator until that stream has passed
+    the call."""
+    if stream is None:
+        return -1, work
+    ptr = _stream(stream) or 0
+    if work is None and need is not None:
+        n = need(*args)
+        if n > 0:
+            work = torch.empty(n, dtype=torch.uint8, device="cuda")
+            if ptr:
+                work.record_stream(torch.cuda.ExternalStream(ptr))
+            else:
+                work.record_stream(torch.cuda.default_stream())
+    return ptr, work
 
 
-def _elem(t, name: str) -> int:
-    """nf_dtype of a GPU tensor on the current device."""
-    code = _elems.get(_tensor(t, name).dtype)
-    if code is None or not t.is_cuda:
-        raise ValueError(f"{name} must be an fp32, bf16 or fp16 GPU tensor")
-    if t.get_device() != _device():
-        raise ValueError(f"{name} is not on the current device")
-    return code
-
-
-def _matrix(t, name: str, shape=None):
-    """(pointer, rows, columns, row pitch) of a 2-D tensor of contiguous rows."""
-    if t.dim() != 2 or (shape is not None and t.shape != shape):
-        raise ValueError(f"{name} must be 2-D" + (f" of shape {tuple(shape)}" if shape else ""))
-    rows, cols = t.shape
-    ld, one = t.stride()
-    if rows <= 1:
-        ld = cols
-    if (one != 1 and cols > 1) or ld < cols:
-        raise ValueError(f"{name}'s rows must be contiguous and apart")
-    return t.data_ptr(), rows, cols, ld
-
-
-def _vector(t, name: str, dtype, shape):
-    """Pointer of a contiguous GPU tensor of this type and shape, None for None."""
-    if t is None:
-        return None
-    if _tensor(t, name).dtype is not dtype or not t.is_cuda or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} GPU tensor of shape {tuple(shape)}")
-    return t.data_ptr()
-
-
-def _queue(stream):
-    if stream is not None:
-        return _stream(stream)
-    return _raw_stream(_device()) or None
-
-
-def _workspace(work, need: int, stream, name: str):
-    """(pointer, bytes, tensor) of the caller's workspace, or of one from torch's
-    allocator, which keeps it until the stream has passed the call."""
-    if need < 0:
-        raise NfError(NF_ESHAPE, name)
-    if work is None:
-        work = torch.empty(need, dtype=torch.uint8, device="cuda")
-        if stream is not None:
-            work.record_stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
-        return work.data_ptr(), need, work
-    if not _tensor(work, "work").is_cuda or not work.is_contiguous():
-        raise ValueError("work must be a contiguous GPU tensor")
-    return work.data_ptr(), work.numel() * work.element_size(), work
+def _code(t) -> int:
+    return {torch.float32: NF_F32, torch.bfloat16: NF_BF16, torch.float16: NF_F16}.get(t.dtype, -1)
 
 
 def nf_logprobs_work(dtype: int, rows: int, classes: int, n_top: int = 0, gradient: bool = False) -> int:
@@ -498,52 +465,28 @@ def nf_logprobs_work(dtype: int, rows: int, classes: int, n_top: int = 0, gradie
     return n
 
 
-def _few_rows(code: int, rows: int, cols: int, n_top: int, gradient: int, work, stream):
-    """The workspace of few long rows; none for others (many or short ones need none)."""
-    if work is None and (rows > 64 or cols < 16384):
-        return None, 0, None
-    need = _lib.nf_logprobs_work(code, rows, cols, n_top, gradient)
-    return _workspace(work, need, stream, "nf_logprobs_work") if need > 0 else (None, 0, None)
-
-
 def nf_logprobs(logits, targets=None, logp=None, entropy=None, stat=None, top_ids=None, top_logp=None,
                 scale: float = 1.0, work=None, stream=None) -> None:
     """logits [rows][classes], targets [rows] int64; logp, entropy [rows], stat
     [rows][2], top_ids (int32) and top_logp [rows][n_top] receive what they name."""
-    code = _elem(logits, "logits")
-    x, rows, cols, ld = _matrix(logits, "logits")
-    top = top_ids if top_ids is not None else top_logp
-    n_top = 0 if top is None else top.shape[-1]
-    row = (rows,)
-    w, n, keep = _few_rows(code, rows, cols, n_top, 0, work, stream)
-    st = _lib.nf_logprobs(x, code, rows, cols, ld, scale, _vector(targets, "targets", _i64_t, row), n_top,
-                          _vector(logp, "logp", _f32_t, row), _vector(entropy, "entropy", _f32_t, row),
-                          _vector(stat, "stat", _f32_t, (rows, 2)), _vector(top_ids, "top_ids", _i32_t, (rows, n_top)),
-                          _vector(top_logp, "top_logp", _f32_t, (rows, n_top)), w, n, _queue(stream))
+    if stream is None:
+        st = _nfbind.logprobs(logits, targets, logp, entropy, stat, top_ids, top_logp, scale, work, -1)
+    else:
+        top = top_ids if top_ids is not None else top_logp
+        s, work = _on(stream, work, lambda: _lib.nf_logprobs_work(_code(logits), *logits.shape,
+                                                                  0 if top is None else top.shape[-1], 0))
+        st = _nfbind.logprobs(logits, targets, logp, entropy, stat, top_ids, top_logp, scale, work, s)
     if st:
         raise NfError(st, "nf_logprobs")
-
-
-def _like(t, of, code: int, name: str):
-    if _elem(t, name) != code:
-        raise ValueError(f"{name} must have the type of the logits")
-    p, _, _, ld = _matrix(t, name, of.shape)
-    return p, ld
 
 
 def nf_logprobs_train(logits, targets, g_logp, g_entropy, dlogits, logp=None, entropy=None, stat=None,
                       scale: float = 1.0, work=None, stream=None) -> None:
     """nf_logprobs with the gradient of sum(g_logp logp + g_entropy entropy) in
     dlogits [rows][classes], which may be the logits."""
-    code = _elem(logits, "logits")
-    x, rows, cols, ld = _matrix(logits, "logits")
-    dx, ldd = _like(dlogits, logits, code, "dlogits")
-    row = (rows,)
-    w, n, keep = _few_rows(code, rows, cols, 0, 1, work, stream)
-    st = _lib.nf_logprobs_train(x, code, rows, cols, ld, scale, _vector(targets, "targets", _i64_t, row),
-                                _vector(g_logp, "g_logp", _f32_t, row), _vector(g_entropy, "g_entropy", _f32_t, row),
-                                _vector(logp, "logp", _f32_t, row), _vector(entropy, "entropy", _f32_t, row),
-                                _vector(stat, "stat", _f32_t, (rows, 2)), dx, ldd, w, n, _queue(stream))
+    s, work = (-1, work) if stream is None else _on(
+        stream, work, lambda: _lib.nf_logprobs_work(_code(logits), *logits.shape, 0, 1))
+    st = _nfbind.logprobs_train(logits, targets, g_logp, g_entropy, dlogits, logp, entropy, stat, scale, work, s)
     if st:
         raise NfError(st, "nf_logprobs_train")
 
@@ -551,31 +494,10 @@ def nf_logprobs_train(logits, targets, g_logp, g_entropy, dlogits, logp=None, en
 def nf_logprobs_grad(logits, targets, stat, entropy, g_logp, g_entropy, dlogits, scale: float = 1.0,
                      stream=None) -> None:
     """The same gradient from the stat (and entropy) of an earlier nf_logprobs."""
-    code = _elem(logits, "logits")
-    x, rows, cols, ld = _matrix(logits, "logits")
-    dx, ldd = _like(dlogits, logits, code, "dlogits")
-    row = (rows,)
-    st = _lib.nf_logprobs_grad(x, code, rows, cols, ld, scale, _vector(targets, "targets", _i64_t, row),
-                               _vector(stat, "stat", _f32_t, (rows, 2)), _vector(entropy, "entropy", _f32_t, row),
-                               _vector(g_logp, "g_logp", _f32_t, row), _vector(g_entropy, "g_entropy", _f32_t, row),
-                               dx, ldd, _queue(stream))
+    st = _nfbind.logprobs_grad(logits, targets, stat, entropy, g_logp, g_entropy, dlogits, scale,
+                               -1 if stream is None else _stream(stream) or 0)
     if st:
         raise NfError(st, "nf_logprobs_grad")
-
-
-def _stack(t, name: str):
-    """(pointer, count, rows, columns, row pitch, matrix pitch) of a matrix or a stack."""
-    if t.dim() not in (2, 3):
-        raise ValueError(f"{name} must be a matrix or a stack of matrices")
-    count = t.shape[0] if t.dim() == 3 else 1
-    stride = t.stride(0) if t.dim() == 3 and count > 1 else 0
-    rows, cols = t.shape[-2:]
-    ld, one = t.stride()[-2:]
-    if rows <= 1:
-        ld = cols
-    if (one != 1 and cols > 1) or ld < cols:
-        raise ValueError(f"{name}'s rows must be contiguous and apart")
-    return t.data_ptr(), count, rows, cols, ld, stride
 
 
 def nf_orthogonalize_work(dtype: int, count: int, rows: int, cols: int) -> int:
@@ -586,32 +508,25 @@ def nf_orthogonalize_work(dtype: int, count: int, rows: int, cols: int) -> int:
     return n
 
 
+def _stack_work(t):
+    return _lib.nf_orthogonalize_work(_code(t), t.shape[0] if t.dim() == 3 else 1, t.shape[-2], t.shape[-1])
+
+
 def nf_orthogonalize(x, out, work=None, stream=None) -> None:
     """x: a matrix [rows][cols] or a stack [count][rows][cols] in fp32 or bf16; out of the
     same type and shape, or x itself."""
-    code = _elem(x, "x")
-    if _elem(out, "out") != code or out.shape != x.shape:
-        raise ValueError("out must have x's type and shape")
-    p, count, rows, cols, ld, stride = _stack(x, "x")
-    o, _, _, _, ldo, so = _stack(out, "out")
-    w, n, keep = _workspace(work, _lib.nf_orthogonalize_work(code, count, rows, cols), stream, "nf_orthogonalize")
-    _check(_lib.nf_orthogonalize(p, code, count, rows, cols, ld, stride, o, ldo, so, w, n, _queue(stream)),
-           "nf_orthogonalize")
+    s, work = (-1, work) if stream is None else _on(stream, work, _stack_work, x)
+    st = _nfbind.orthogonalize(x, out, work, s)
+    if st:
+        raise NfError(st, "nf_orthogonalize")
 
 
 def nf_muon_step(w, m, g, w_out, m_out, eta: float, momentum: float = 0.95, nesterov: bool = True,
                  decay: float = 0.0, work=None, stream=None) -> None:
     """One step on w ([rows][cols] or a stack) with gradient g and fp32 momentum m, into
     w_out and m_out (which may be w and m).  All contiguous."""
-    wc, gc = _elem(w, "w"), _elem(g, "g")
-    shape = w.shape
-    _, count, rows, cols, _, _ = _stack(w, "w")
-    wp, gp = _vector(w, "w", w.dtype, shape), _vector(g, "g", g.dtype, shape)
-    mp, wo = _vector(m, "m", _f32_t, shape), _vector(w_out, "w_out", w.dtype, shape)
-    mo = _vector(m_out, "m_out", _f32_t, shape)
-    k, n, keep = _workspace(work, _lib.nf_orthogonalize_work(wc, count, rows, cols), stream, "nf_muon_step")
-    st = _lib.nf_muon_step(wp, wc, mp, gp, gc, count, rows, cols, eta, momentum, int(nesterov), decay, wo, mo, k, n,
-                           _queue(stream))
+    s, work = (-1, work) if stream is None else _on(stream, work, _stack_work, w)
+    st = _nfbind.muon_step(w, m, g, w_out, m_out, eta, momentum, nesterov, decay, work, s)
     if st:
         raise NfError(st, "nf_muon_step")
 
@@ -620,22 +535,10 @@ def _act(act) -> int:
     return NF_NO_ACT if act is None else ACT_CODES[act] if isinstance(act, str) else int(act)
 
 
-def _bytes_matrix(t, name: str):
-    if _tensor(t, name).dtype is not _i8_t or not t.is_cuda:
-        raise ValueError(f"{name} must be an int8 GPU tensor")
-    return _matrix(t, name)
-
-
 def nf_quantize_rows(x, q, scale, stream=None) -> None:
     """x [rows][cols] into int8 q [rows][cols up to a multiple of 16, or more] and fp32
     scale [rows]."""
-    code = _elem(x, "x")
-    p, rows, cols, ld = _matrix(x, "x")
-    qp, qrows, wide, ldq = _bytes_matrix(q, "q")
-    if qrows != rows or wide < (cols + 15) // 16 * 16:
-        raise ValueError("q must have x's rows and columns, these up to a multiple of 16")
-    st = _lib.nf_quantize_rows(p, code, rows, cols, ld, qp, ldq, _vector(scale, "scale", _f32_t, (rows,)),
-                               _queue(stream))
+    st = _nfbind.quantize_rows(x, q, scale, -1 if stream is None else _stream(stream) or 0)
     if st:
         raise NfError(st, "nf_quantize_rows")
 
@@ -643,17 +546,8 @@ def nf_quantize_rows(x, q, scale, stream=None) -> None:
 def nf_linear_i8(xq, x_scale, wq, w_scale, y, inputs: int, bias=None, act=None, stream=None) -> None:
     """y [rows][outputs] = act(x_scale w_scale (xq wq^T) + bias) of rows and weights
     as nf_quantize_rows leaves them (int8 [..][inputs up to a multiple of 16])."""
-    xp, rows, xw, ldx = _bytes_matrix(xq, "xq")
-    wp, outs, ww, ldw = _bytes_matrix(wq, "wq")
-    wide = (inputs + 15) // 16 * 16
-    if xw < wide or ww < wide:
-        raise ValueError("xq and wq must hold the inputs, up to a multiple of 16")
-    yc = _elem(y, "y")
-    yp, _, _, ldy = _matrix(y, "y", (rows, outs))
-    out = (outs,)
-    st = _lib.nf_linear_i8(xp, ldx, _vector(x_scale, "x_scale", _f32_t, (rows,)), wp, ldw,
-                           _vector(w_scale, "w_scale", _f32_t, out), _vector(bias, "bias", _f32_t, out), _act(act),
-                           rows, inputs, outs, yp, yc, ldy, _queue(stream))
+    st = _nfbind.linear_i8(xq, x_scale, wq, w_scale, y, inputs, bias, _act(act),
+                           -1 if stream is None else _stream(stream) or 0)
     if st:
         raise NfError(st, "nf_linear_i8")
 
@@ -668,17 +562,8 @@ def nf_linear_i8_work(rows: int, inputs: int) -> int:
 
 def nf_linear_i8_dynamic(x, wq, w_scale, y, bias=None, act=None, work=None, stream=None) -> None:
     """nf_linear_i8 of the rows x [rows][inputs], which it quantises."""
-    code, yc = _elem(x, "x"), _elem(y, "y")
-    xp, rows, cols, ldx = _matrix(x, "x")
-    wp, outs, ww, ldw = _bytes_matrix(wq, "wq")
-    if ww < (cols + 15) // 16 * 16:
-        raise ValueError("wq must hold x's columns, up to a multiple of 16")
-    yp, _, _, ldy = _matrix(y, "y", (rows, outs))
-    out = (outs,)
-    ws, bs = _vector(w_scale, "w_scale", _f32_t, out), _vector(bias, "bias", _f32_t, out)
-    k, n, keep = _workspace(work, _lib.nf_linear_i8_work(rows, cols), stream, "nf_linear_i8_dynamic")
-    st = _lib.nf_linear_i8_dynamic(xp, code, ldx, wp, ldw, ws, bs, _act(act), rows, cols, outs, yp, yc, ldy, k, n,
-                                   _queue(stream))
+    s, work = (-1, work) if stream is None else _on(stream, work, lambda: _lib.nf_linear_i8_work(*x.shape))
+    st = _nfbind.linear_i8_dynamic(x, wq, w_scale, y, bias, _act(act), work, s)
     if st:
         raise NfError(st, "nf_linear_i8_dynamic")
 
