@@ -181,6 +181,23 @@ __global__ void __launch_bounds__(256) orth_fill_kernel(const FillArgs<T> a) {
   __shared__ float tile[64][65];
   __shared__ double part[4];
   const int tid = threadIdx.x;
+  const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;
+  const T* const g = a.g.p + (int64_t)blockIdx.z * a.g.stride;
+  const float* const mom = a.m.p ? a.m.p + (int64_t)blockIdx.z * a.m.stride : nullptr;
+  // The loads of a thread's values are under way together, and with those of the sums
+  // (lanes along the user's rows; places past the matrix read its first value instead).
+  constexpr int N = 64 * 64 / 256;
+  T u[N];
+  float m[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const int e = k * 256 + tid, c = e & 63, r = e >> 6;
+    const int i = i0 + (a.turned ? c : r), j = j0 + (a.turned ? r : c);
+    const bool in = i < p.m && j < p.n;
+    const int64_t ur = in ? a.turned ? j : i : 0, uc = in ? a.turned ? i : j : 0;
+    u[k] = g[ur * a.g.ld + uc];
+    m[k] = mom ? mom[ur * a.m.ld + uc] : 0.f;
+  }
   double s = 0.0;
   for (int i = tid; i < a.blocks; i += 256) s += reinterpret_cast<const double*>(w + p.sums)[i];
   s = wave_sum(s);
@@ -189,32 +206,15 @@ __global__ void __launch_bounds__(256) orth_fill_kernel(const FillArgs<T> a) {
   const double sum = (part[0] + part[1]) + (part[2] + part[3]);
   // a matrix of zeros stays one; one that is not finite becomes NaN throughout
   const double inv = sum == 0.0 ? 0.0 : sum < __builtin_inf() ? (double)UNIT / sqrt(sum) : __builtin_nan("");
-  const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;
-  const T* const g = a.g.p + (int64_t)blockIdx.z * a.g.stride;
-  const float* const mom = a.m.p ? a.m.p + (int64_t)blockIdx.z * a.m.stride : nullptr;
 #pragma unroll
-  for (int e0 = 0; e0 < 64 * 64; e0 += 8 * 256) {
-    // lanes along the user's rows; the loads of 8 values are under way together
-    // (places past the matrix read its first value instead)
-    float u[8], m[8];
-    bool in[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int e = e0 + k * 256 + tid, c = e & 63, r = e >> 6;
-      const int i = i0 + (a.turned ? c : r), j = j0 + (a.turned ? r : c);
-      in[k] = i < p.m && j < p.n;
-      const int64_t ur = in[k] ? a.turned ? j : i : 0, uc = in[k] ? a.turned ? i : j : 0;
-      u[k] = to_float(g[ur * a.g.ld + uc]);
-      if (mom) m[k] = mom[ur * a.m.ld + uc];
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int e = e0 + k * 256 + tid, c = e & 63, r = e >> 6;
-      if (mom) u[k] = direction(u[k], m[k], a.momentum, a.nesterov);
-      const float v = !in[k] ? 0.f : inv != inv ? __builtin_nanf("") : (float)((double)u[k] * inv);
-      if (a.turned) tile[c][r] = v;
-      else tile[r][c] = v;
-    }
+  for (int k = 0; k < N; ++k) {
+    const int e = k * 256 + tid, c = e & 63, r = e >> 6;
+    const int i = i0 + (a.turned ? c : r), j = j0 + (a.turned ? r : c);
+    float x = to_float(u[k]);
+    if (mom) x = direction(x, m[k], a.momentum, a.nesterov);
+    const float v = !(i < p.m && j < p.n) ? 0.f : inv != inv ? __builtin_nanf("") : (float)((double)x * inv);
+    if (a.turned) tile[c][r] = v;
+    else tile[r][c] = v;
   }
   __syncthreads();
   const int nx = p.kx / (KIND == MM_PARTS2 ? 4 : 2), nt = p.kt / (KIND == MM_PARTS2 ? 4 : 2);
