@@ -175,7 +175,7 @@ PyObject* logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
       if (a[k] != Py_None) top = tensor(a[k], "top").dim() ? THPVariable_Unpack(a[k]).size(-1) : 0;
     if (top > NF_TOP_MAX) top = NF_TOP_MAX + 1;            // refused below
     Work w;
-    if (m.rows <= 64) w.take(a[8], nf_logprobs_work(code, m.rows, m.cols < 1 ? 1 : m.cols, (int)(top > NF_TOP_MAX ? 0 : top), 0), x);
+    w.take(a[8], nf_logprobs_work(code, m.rows, m.cols < 1 ? 1 : m.cols, (int)(top > NF_TOP_MAX ? 0 : top), 0), x);
     return call(nf_logprobs, m.p, code, m.rows, m.cols, m.ld, (float)number(a[7]),
                        (const int64_t*)vector(a[1], "targets", at::kLong, {m.rows}), (int)top,
                        (float*)vector(a[2], "logp", at::kFloat, {m.rows}),
@@ -199,7 +199,7 @@ PyObject* logprobs_train(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int code = elem(x, "logits");
     const Matrix m = matrix(x, "logits"), d = gradient(a[4], code, m);
     Work w;
-    if (m.rows <= 64) w.take(a[9], nf_logprobs_work(code, m.rows, m.cols < 1 ? 1 : m.cols, 0, 1), x);
+    w.take(a[9], nf_logprobs_work(code, m.rows, m.cols < 1 ? 1 : m.cols, 0, 1), x);
     return call(nf_logprobs_train, m.p, code, m.rows, m.cols, m.ld, (float)number(a[8]),
                              (const int64_t*)vector(a[1], "targets", at::kLong, {m.rows}),
                              (const float*)vector(a[2], "g_logp", at::kFloat, {m.rows}),

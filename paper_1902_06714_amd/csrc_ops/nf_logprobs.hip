@@ -571,20 +571,27 @@ struct GradArgs {
   const float* h;
 };
 
-constexpr int GRAD_VECS = 4;
+constexpr int GRAD_VECS = 2;
 
-template <class T>
+// L threads a row and GRAD_VECS vectors each, or of longer rows 256 and several
+// workgroups a row.  Bound by the bytes (16000 x 2000 bf16 32 us, 4.0 TB/s); us by 256 threads
+// and by the fewest that hold a row: 16000 x 10 f32 12.2, 3.3; x 100 f32 13.6, 5.1; x 500 bf16
+// 16.9, 13.1.  Vectors a thread, 4, 2, 1: 16000 x 2000 bf16 38.7, 32.1, 33.0; 1001 x 5003 f32
+// 12.0, 9.5, 9.2.
+template <class T, int L>
 __global__ void __launch_bounds__(256) logp_grad_kernel(const GradArgs<T> a) {
   constexpr int E = Vec16<T>::N;
-  const int64_t row = blockIdx.x / a.per_row;
-  const int first = (int)(blockIdx.x - row * a.per_row) * 256 * E * GRAD_VECS;
+  const int64_t row = L == 256 ? blockIdx.x / a.per_row : (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
+  if (row >= a.rows) return;
+  const int first = L == 256 ? (int)(blockIdx.x - row * a.per_row) * 256 * E * GRAD_VECS : 0;
+  const int lane = threadIdx.x % L;
   const int V = a.classes;
   const T* const x = a.x + row * a.ld;
   T* const dx = a.dx + row * a.ld_dx;
   Vec16<T> v[GRAD_VECS];
 #pragma unroll
   for (int u = 0; u < GRAD_VECS; ++u) {
-    const int j = first + (u * 256 + (int)threadIdx.x) * E;
+    const int j = first + (u * L + lane) * E;
     if (j + E <= V) {
       v[u] = load16(x + j);
     } else {
@@ -603,7 +610,7 @@ __global__ void __launch_bounds__(256) logp_grad_kernel(const GradArgs<T> a) {
   with_share(sl, [&](auto eh) {
 #pragma unroll
     for (int u = 0; u < GRAD_VECS; ++u) {
-      const int j = first + (u * 256 + (int)threadIdx.x) * E;
+      const int j = first + (u * L + lane) * E;
       if (j < V) put_slope<eh.value>(sl, v[u], a.scale, dx, j, V, t);
     }
   });
@@ -617,7 +624,9 @@ struct LogpPlan {
 };
 // Few long rows would leave most of the card idle: they are cut so that about 256
 // workgroups have 16 KB or more each.  Another launch or two costs about 4 us each, so rows
-// stay whole below 96 KB, with a gradient below 256 KB (us, cut and whole: see launch_logp).
+// stay whole below 96 KB, with a gradient below 256 KB (us, cut and whole: 1 x 131072 f32
+// 10.3, 20, with its gradient 9.8, 29; 20 x 50000 f32 11.1, 15), and 65 or more always (100 x 131072
+// f16 with 20 alternatives 23.7, 24.1; 100 x 50000 f32 16.8, 12.7; 128 x 131072 f32 17.2, 15.8).
 LogpPlan logp_plan(int64_t size, int64_t rows, int64_t classes, int n_top, bool grad) {
   LogpPlan p;
   const int64_t bytes = classes * size;
@@ -654,9 +663,13 @@ hipError_t launch_parts(LogpArgs<T> a, const LogpPlan& p, char* work, hipStream_
 
 template <class T>
 hipError_t launch_grad(GradArgs<T> a, hipStream_t s) {
-  constexpr int64_t per = 256 * Vec16<T>::N * GRAD_VECS;
-  a.per_row = (int)((a.classes + per - 1) / per);
-  return op_launch(logp_grad_kernel<T>, dim3((unsigned)(a.rows * a.per_row)), dim3(256), s, a);
+  constexpr int64_t per = Vec16<T>::N * GRAD_VECS;        // of a thread
+  auto blocks = [&](int64_t lanes) { return dim3((unsigned)((a.rows + 256 / lanes - 1) / (256 / lanes))); };
+  a.per_row = (int)((a.classes + 256 * per - 1) / (256 * per));
+  if (a.classes <= 4 * per) return op_launch(logp_grad_kernel<T, 4>, blocks(4), dim3(256), s, a);
+  if (a.classes <= 16 * per) return op_launch(logp_grad_kernel<T, 16>, blocks(16), dim3(256), s, a);
+  if (a.classes <= 64 * per) return op_launch(logp_grad_kernel<T, 64>, blocks(64), dim3(256), s, a);
+  return op_launch(logp_grad_kernel<T, 256>, dim3((unsigned)(a.rows * a.per_row)), dim3(256), s, a);
 }
 
 template <class T, bool GRAD>
