@@ -236,13 +236,13 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * G * 64, OCC) linear_ke
   });
 }
 
-template <class T, int BM, int WM, int WN, int NS, int G, int OCC>
+template <class T, int BM, int WM, int WN, int NS, int G, int OCC, int BN = BM>
 hipError_t launch_linear_tile(LinearArgs a, hipStream_t s) {
   a.mt = (a.rows + BM - 1) / BM;
-  a.nt = (a.outputs + BM - 1) / BM;
+  a.nt = (a.outputs + BN - 1) / BN;
   a.total = a.mt * a.nt;
-  return op_launch(linear_kernel<T, BM, BM, WM, WN, NS, G, OCC>, dim3(mm_grid(a.total)),
-                  dim3((BM / WM) * (BM / WN) * G * 64), s, a);
+  return op_launch(linear_kernel<T, BM, BN, WM, WN, NS, G, OCC>, dim3(mm_grid(a.total)),
+                  dim3((BM / WM) * (BN / WN) * G * 64), s, a);
 }
 
 // ---- few rows: the weights' bytes ----------------------------------------------
@@ -405,7 +405,13 @@ hipError_t launch_linear_as(const LinearArgs& a, int units, hipStream_t s) {
   switch (mm_shape(tiles, units, (a.bytes + MM_STAGE - 1) / MM_STAGE)) {
     case MM_64_GROUPS: return launch_linear_tile<T, 64, 32, 32, 3, 2, 2>(a, s);
     case MM_64: return launch_linear_tile<T, 64, 32, 32, 3, 1, 3>(a, s);
-    case MM_128: return launch_linear_tile<T, 128, 64, 32, 2, 1, 4>(a, s);
+    case MM_128:
+      // 128 x 192 where all tiles run at once then, two on a compute unit (us, 128 and 192 columns: 784
+      // inputs 10000 x 1024 f32 25.3, 23.2, bf16 25.8, 24.8; 300, 16000 x 600 21.6, 21.2; 100, 14000 x 700
+      // 20.2, 19.7)
+      if (tiles(128) > 2 * units && ((a.rows + 127) / 128) * ((a.outputs + 191) / 192) <= 2 * units)
+        return launch_linear_tile<T, 128, 64, 96, 2, 1, 2, 192>(a, s);
+      return launch_linear_tile<T, 128, 64, 32, 2, 1, 4>(a, s);
     case MM_192: return launch_linear_tile<T, 192, 96, 96, 3, 1, 1>(a, s);
     default: return launch_linear_tile<T, 256, 128, 64, 2, 1, 2>(a, s);
   }
