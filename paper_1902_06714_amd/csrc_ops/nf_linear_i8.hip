@@ -4,6 +4,11 @@
 //
 // Sums are whole numbers in 32 bits and exact: NF_LINEAR_I8_MAX inputs times
 // 128 x 128 stay below 2^31.
+//
+// What bounds it, measured with the quantisation (us): the matrix cores for 8192 rows, 4096
+// inputs and outputs in bf16, 156 (the product alone 140, 1.96 POP/s); the outputs' and
+// operands' bytes, one after the other, for 10000 x 784 to 1024 in fp32, 31; the weights' bytes
+// for one row of 4096 to 4096, 7.3 (2.3 TB/s; 3.5 of it the launch).
 #include "nf_act.h"
 #include "rows_mm.h"
 

@@ -9,7 +9,10 @@
 // where they hold it (up to 128 KB), so that the maximum, the sums, the
 // alternatives and the gradient all come from one read; a longer row is read
 // with a running maximum and sum, and again for each of the others.  Rows of at
-// most 128 classes take 8 to 64 lanes of a wave.
+// most 128 classes take 8 to 64 lanes of a wave.  Measured (us): the loss with its gradient
+// of 4096 x 32768 bf16 114 (4.7 TB/s, a copy 5.0); scores of 2049 x 50021 bf16 with 8
+// alternatives 72 (2.8 TB/s: about 13 vector instructions a value beside an exponential bound
+// it); 10000 x 10 f32 4.3 and 1 x 32768 bf16 7.5 (a launch alone takes 3.5).
 //
 // Alternatives: ordered(z) is a whole number in z's order, so (ordered(z),
 // ~index) orders by value and then by the lower index, and no two are equal.
