@@ -408,6 +408,7 @@ template <class T>
 hipError_t launch_linear_as(const LinearArgs& a, int units, hipStream_t s) {
   auto tiles = [&](int64_t b) { return ((a.rows + b - 1) / b) * ((a.outputs + b - 1) / b); };
   switch (mm_shape(tiles, units, (a.bytes + MM_STAGE - 1) / MM_STAGE)) {
+    case MM_32_GROUPS: return launch_linear_tile<T, 32, 32, 32, 3, 4, 1>(a, s);
     case MM_64_GROUPS: return launch_linear_tile<T, 64, 32, 32, 3, 2, 2>(a, s);
     case MM_64: return launch_linear_tile<T, 64, 32, 32, 3, 1, 3>(a, s);
     case MM_128:

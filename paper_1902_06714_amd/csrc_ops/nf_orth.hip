@@ -62,7 +62,7 @@ __device__ __forceinline__ void put_four(char* p, int64_t at, const float (&x)[4
 // bytes).
 struct OrthPlan {
   int m, n;                   // shorter and longer side
-  int kx, kt;                 // bytes of a row of n, of m, whole stages, the last with zeros
+  int kx, kt;                 // bytes of a row of n, in whole stages, and of m, in whole tiles of 32; zeros past the last
   int64_t px, pt, pm;         // pitches of rows of n, of rows of m, of the fp32 X
   int64_t x, xt[2], a, b, xm, da, db, sums;
   int64_t bytes;              // of one matrix
@@ -80,7 +80,7 @@ OrthPlan orth_plan(bool parts, int64_t rows, int64_t cols) {
   p.m = (int)(rows < cols ? rows : cols);
   p.n = (int)(rows < cols ? cols : rows);
   p.kx = (int)up((int64_t)p.n * (parts ? 4 : 2), 128);
-  p.kt = (int)up((int64_t)p.m * (parts ? 4 : 2), 128);
+  p.kt = (int)up((int64_t)p.m * (parts ? 4 : 2), parts ? 128 : 64);
   p.px = odd_pitch(p.kx);
   p.pt = odd_pitch(p.kt);
   p.pm = parts ? 0 : odd_pitch(2 * (int64_t)p.kx);
@@ -514,6 +514,7 @@ hipError_t launch_product(const MmArgs& a, int64_t count, int units, hipStream_t
   };
   const int64_t bytes = PROD == PROD_GRAM ? a.p.kx : a.p.kt;
   switch (mm_shape(tiles, units, (bytes + MM_STAGE - 1) / MM_STAGE)) {
+    case MM_32_GROUPS: return launch_tile<KIND, PROD, 32, 32, 32, 3, 4, 1>(a, count, s);
     case MM_64_GROUPS: return launch_tile<KIND, PROD, 64, 32, 32, 3, 2, 2>(a, count, s);
     case MM_64: return launch_tile<KIND, PROD, 64, 32, 32, 3, 1, 3>(a, count, s);
     case MM_128: return launch_tile<KIND, PROD, 128, 64, 32, 2, 1, 4>(a, count, s);

@@ -321,7 +321,10 @@ __device__ __forceinline__ bool mm_place_lower(int total, int& bx, int& by) {
 }
 
 // The tile of a product: tiles(B) of B x B on a card of `units` compute units.
-// Measured (us; X' = a X + B X of m x m in pairs of parts, and in one f16 where two are given):
+// Tiles of 32 by four groups of waves where each has a compute unit of its own, which takes
+// in half the operands' bytes then (us, 64 by two groups and 32, launches included: X X^T of 203 x 3210 in pairs
+// 20.2, 13.1, of 300 x 700 8.7, 6.4; a X + B X of 300 x 700 7.6, 6.7; 8-bit, 17 rows of 5000 to 700
+// 11.0, 7.6, 200 of 2900 to 500 9.3, 6.3).  Larger tiles, measured (us; X' = a X + B X of m x m in pairs of parts, and in one f16 where two are given):
 //   m       64, two groups   64, one     128         256
 //   768     11.0 / 9.1       11.3 / 9.1  23.0 / 14.4 60.1 / 31.1    144 tiles of 64
 //   1024    13.4 / 10.0      14.5 / 10.6 27.8 / 17.2 74.1 / 35.8    256
@@ -333,9 +336,10 @@ __device__ __forceinline__ bool mm_place_lower(int total, int& bx, int& by) {
 // entries times its stages and 6 for its end; a stage of the smaller ones takes 1.1 and 1.2
 // times as long for its entries, and the end of one of 128 runs beside another's stages
 // (8-bit products of 10000 x 1024 over 7 stages: 128 25.3, 256 28.0; 8192 x 4096 over 32: 174, 143).
-enum MmShape { MM_64_GROUPS, MM_64, MM_128, MM_192, MM_256 };
+enum MmShape { MM_32_GROUPS, MM_64_GROUPS, MM_64, MM_128, MM_192, MM_256 };
 template <class F>
 inline MmShape mm_shape(F&& tiles, int64_t units, int64_t stages) {
+  if (tiles(32) <= units) return MM_32_GROUPS;
   const int64_t small = tiles(64);
   if (small <= units) return MM_64_GROUPS;
   if (small <= 3 * units) return MM_64;

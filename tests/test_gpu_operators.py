@@ -344,6 +344,13 @@ def test_orthogonalize_larger_tiles(rows, cols, dtype):
     assert off <= (2e-5 if dtype == "f32" else 6e-3), off
 
 
+# products of one call in tiles of 32 and of 64, the shorter side no whole tile of either
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(593, 641), (577, 800), (70, 4000), (225, 2100)])
+def test_orthogonalize_mixed_tiles(rows, cols, dtype):
+    test_orthogonalize(rows, cols, dtype)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_orthogonalize_stacks_and_values(dtype):
     """Matrices of a stack do not see one another: one of zeros, one with a NaN, one
@@ -499,6 +506,13 @@ def test_linear_activations(act, rows):
 @pytest.mark.parametrize("rows,inputs,outputs", [(2100, 300, 2080), (4200, 129, 4100), (8200, 64, 2050)])
 def test_linear_larger_tiles(rows, inputs, outputs):
     _linear_case(rows, inputs, outputs, "bf16", "f32", "relu", True, 3)
+
+
+# tiles of 64 by two groups of waves, of 64, and of 128 x 192, each past its edges
+@pytest.mark.parametrize("rows,inputs,outputs", [(700, 300, 901), (1501, 129, 1300), (4200, 250, 2101)])
+@pytest.mark.parametrize("y_dtype", ["f32", "f16"])
+def test_linear_middle_tiles(rows, inputs, outputs, y_dtype):
+    _linear_case(rows, inputs, outputs, "f32", y_dtype, "tanh", True, 1)
 
 
 @pytest.mark.parametrize("rows", [1, 3, 40, 300])
