@@ -436,20 +436,20 @@ else:
 
 
 def _on(stream, work, need, *args):
-    """(stream for _nfbind, workspace): the current stream's workspace comes from there;
-    on another stream it is kept by torch's allocator until that stream has passed
-    the call."""
+    """(stream for _nfbind, workspace).  The current stream's workspace comes from there;
+    one for another stream is allocated on that stream: memory that torch's allocator
+    hands to the current stream may still be in use by what was put there before."""
     if stream is None:
         return -1, work
     ptr = _stream(stream) or 0
-    if work is None and need is not None:
-        n = need(*args)
-        if n > 0:
-            work = torch.empty(n, dtype=torch.uint8, device="cuda")
-            if ptr:
-                work.record_stream(torch.cuda.ExternalStream(ptr))
-            else:
-                work.record_stream(torch.cuda.default_stream())
+    if work is None:
+        try:
+            n = need(*args)
+        except (AttributeError, IndexError, TypeError, ctypes.ArgumentError):
+            n = 0                       # no such tensors: refused by the call
+        if n > 0 and torch.cuda.is_available():
+            with torch.cuda.stream(torch.cuda.ExternalStream(ptr) if ptr else torch.cuda.default_stream()):
+                work = torch.empty(n, dtype=torch.uint8, device="cuda")
     return ptr, work
 
 

@@ -604,6 +604,27 @@ def test_a_stream_of_its_own():
         assert torch.equal(o, e)
 
 
+def test_workspace_belongs_to_the_stream(monkeypatch):
+    """A workspace for another stream is that stream's memory from the beginning."""
+    torch, nf = torch_cuda(), _nf()
+    note("workspace of another stream")
+    x, out = torch.randn(70, 90, device="cuda"), torch.empty(70, 90, device="cuda")
+    torch.cuda.synchronize()
+    side, seen, empty = torch.cuda.Stream(), [], torch.empty
+
+    def watched(*a, **k):
+        seen.append(torch.cuda.current_stream().cuda_stream)
+        return empty(*a, **k)
+
+    monkeypatch.setattr(torch, "empty", watched)
+    nf.nf_orthogonalize(x, out, stream=side)
+    monkeypatch.undo()
+    torch.cuda.synchronize()
+    assert seen == [side.cuda_stream]
+    want = ref.orthogonalize(_np(x))
+    assert np.linalg.norm(_np(out) - want) <= 2e-5 * np.linalg.norm(want)
+
+
 def test_captured_in_a_graph():
     torch = torch_cuda()
     go, ins, outs = _all_calls(6)

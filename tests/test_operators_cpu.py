@@ -202,3 +202,14 @@ def test_tensors_must_be_on_the_gpu():
         nf.nf_orthogonalize(x, x)
     with pytest.raises(TypeError):
         nf.nf_logprobs([1.0])
+
+
+def test_tensors_for_another_stream_must_be_on_the_gpu():
+    import torch
+    with pytest.raises(ValueError):
+        nf.nf_orthogonalize(torch.zeros(70, 80), torch.zeros(70, 80), stream=0)
+    with pytest.raises(ValueError):
+        nf.nf_orthogonalize(torch.zeros(70), torch.zeros(70), stream=0)
+    for bad in ([1.0], None):
+        with pytest.raises(TypeError):
+            nf.nf_logprobs(bad, stream=0)
