@@ -392,7 +392,8 @@ nf_status nf_logprobs_grad(const void* d_logits, int32_t dtype, int64_t rows, in
  * infinity gives NaN throughout.
  * dtype: NF_F32 (products with fp32's precision) or NF_BF16 (products of fp16
  * values, sums and X itself in fp32).  ld (at most NF_ORTH_MAX_LD) and stride: elements from
- * row to row and from matrix to matrix; d_out may be d_x.
+ * row to row and from matrix to matrix; d_out may be d_x with the same pitch and
+ * stride, or share no element with it.
  * d_work: nf_orthogonalize_work(dtype, count, rows, cols) bytes (-1 for sizes
  * that the call would refuse) aligned to 256. */
 #define NF_ORTH_MAX 65536

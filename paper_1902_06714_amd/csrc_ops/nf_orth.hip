@@ -698,6 +698,13 @@ nf_status nf_orthogonalize(const void* d_x, int32_t dtype, int64_t count, int64_
   if (st != NF_OK) return st;
   if (count > 1 && (stride < 0 || stride_out < (rows - 1) * ld_out + cols))
     return op_fail(NF_ESHAPE, "the results overlap one another");
+  if (count == 1) stride = stride_out = 0;
+  if (stride > INT64_MAX / 8 / count || stride_out > INT64_MAX / 8 / count)
+    return op_fail(NF_ESHAPE, "the matrices times their stride do not fit");
+  // matrices of at most ORTH_SMALL rows or columns are read again while results are written
+  const OpArray x{d_x, count, stride * e, rows, ld * e, cols * e};
+  const OpArray out{d_out, count, stride_out * e, rows, ld_out * e, cols * e};
+  if (op_share(x, out) && !op_same(x, out)) return op_fail(NF_EINVAL, "the result overlaps the matrices without being them");
   OrthCall c{};
   c.count = count;
   c.rows = rows;

@@ -132,6 +132,45 @@ inline bool op_overlap(const void* a, int64_t na, const void* b, int64_t nb) {
   return a && b && na > 0 && nb > 0 && x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
 }
 
+// An array of rows in memory, in bytes: `count` matrices of `rows` rows of `width`.
+struct OpArray {
+  const void* p;
+  int64_t count, stride, rows, pitch, width;
+  // one row a matrix is one matrix of such rows; what is never stepped over does not count
+  OpArray plain() const {
+    OpArray a = *this;
+    if (a.rows == 1) a.rows = a.count, a.pitch = a.stride, a.count = 1;
+    if (a.count == 1) a.stride = 0;
+    if (a.rows == 1) a.pitch = a.width;
+    return a;
+  }
+  int64_t matrix() const { return (rows - 1) * pitch + width; }
+  int64_t span() const { return (count - 1) * stride + matrix(); }
+  bool even() const { return pitch > 0 && stride % pitch == 0; }     // every row is whole pitches from the first
+};
+
+// Whether the rows of two arrays may share bytes.  Arrays that lie side by side in the
+// rows of one buffer, or by turns in one stack, do not.
+inline bool op_share(const OpArray& x, const OpArray& y) {
+  const OpArray a = x.plain(), b = y.plain();
+  if (!op_overlap(a.p, a.span(), b.p, b.span())) return false;
+  const int64_t apart = (int64_t)(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p));
+  // pieces of na bytes and of nb bytes, all of them whole multiples of `step` apart
+  auto by_turns = [](int64_t apart, int64_t step, int64_t na, int64_t nb) {
+    const int64_t d = (apart % step + step) % step;
+    return d >= na && step - d >= nb;
+  };
+  if (a.stride > 0 && a.stride == b.stride && by_turns(apart, a.stride, a.matrix(), b.matrix())) return false;
+  if (a.even() && b.even() && a.pitch == b.pitch && by_turns(apart, a.pitch, a.width, b.width)) return false;
+  return true;
+}
+// Whether they are the same array.
+inline bool op_same(const OpArray& x, const OpArray& y) {
+  const OpArray a = x.plain(), b = y.plain();
+  return a.p == b.p && a.count == b.count && a.stride == b.stride && a.rows == b.rows && a.pitch == b.pitch &&
+         a.width == b.width;
+}
+
 // Calls f with a value of the element type `dtype` names.
 template <class F>
 auto with_type(int dtype, F&& f) {

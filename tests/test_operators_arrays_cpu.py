@@ -1,0 +1,89 @@
+"""Which arrays the operators' entry points take together, which needs no GPU: calls
+that they refuse return before anything is launched, and the rule itself
+(csrc_ops/ops_common.h) is checked against sets of bytes."""
+
+import itertools
+import os
+import subprocess
+
+import pytest
+
+from paper_1902_06714_amd import build, nf
+
+from .test_operators_cpu import E, ORTH, P, _call
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+# d_out over d_x with another pitch or stride, shifted, or a stack that begins at its one input
+@pytest.mark.parametrize("change", [
+    {"x": P, "out": P, "ld": 9},                                                    # the rows move
+    {"x": P, "out": P + 4}, {"x": P + 32, "out": P}, {"x": P, "out": P + 4 * 48},    # shifted
+    {"x": P, "out": P, "stride": 0},                                                # one input of a stack
+    {"x": P, "out": P, "stride": 49},
+    {"x": P, "out": P + 4 * 4, "ld": 16, "ldo": 16, "stride": 96, "so": 96},         # half of the columns
+    {"x": P, "out": P + 4 * 8, "ld": 16, "ldo": 17, "stride": 96, "so": 102},
+    {"x": P, "out": P, "count": 1, "rows": 40, "cols": 70, "ld": 77, "ldo": 70},
+    {"x": P, "out": P, "count": 1, "rows": 300, "cols": 400, "ld": 410, "ldo": 400}])
+def test_orthogonalize_refuses_a_result_over_its_matrices(change):
+    assert _call("nf_orthogonalize", ORTH, change) == E, nf.nf_last_error()
+    assert "overlaps" in nf.nf_last_error()
+
+
+RULE = r"""
+#include <cstdio>
+#include "ops_common.h"
+int main() {
+  long long v[2][6];
+  for (;;) {
+    for (auto& r : v)
+      for (auto& x : r)
+        if (std::scanf("%lld", &x) != 1) return 0;
+    auto of = [](const long long* q) {
+      return nf::OpArray{reinterpret_cast<const void*>(q[0]), q[1], q[2], q[3], q[4], q[5]};
+    };
+    std::printf("%d %d\n", (int)nf::op_share(of(v[0]), of(v[1])), (int)nf::op_same(of(v[0]), of(v[1])));
+  }
+}
+"""
+
+
+def _bytes(p, count, stride, rows, pitch, width):
+    return {p + k * stride + r * pitch + c for k in range(count) for r in range(rows) for c in range(width)}
+
+
+@pytest.fixture(scope="module")
+def rule(tmp_path_factory):
+    d = tmp_path_factory.mktemp("rule")
+    (d / "rule.hip").write_text(RULE)
+    subprocess.run([build.hipcc(), "--offload-arch=gfx950", "-O1", "-std=c++17", "-I", os.path.join(ROOT, "include"),
+                    "-I", build.CSRC, "-I", build.OPS, str(d / "rule.hip"), "-o", str(d / "rule")], check=True)
+
+    def ask(pairs):
+        text = "\n".join(" ".join(str(v) for v in a + b) for a, b in pairs)
+        out = subprocess.run([str(d / "rule")], input=text, capture_output=True, text=True, check=True).stdout
+        return [tuple(map(int, line.split())) for line in out.splitlines()]
+    return ask
+
+
+def test_arrays_that_share_bytes_are_found(rule):
+    """No two arrays with a common byte pass, and those that lie side by side in a
+    buffer's rows, or by turns in a stack, do."""
+    firsts = [(1000, c, s, r, p, w) for c, s in ((1, 0), (2, 0), (2, 64), (3, 70), (3, 64)) for r in (1, 3) for p in (8, 16)
+              for w in (3, 8)]
+    pairs = [((q, *a[1:]), (1000 + off, *b[1:])) for a, b in itertools.product(firsts, firsts)
+             for off, q in ((-20, 1000), (0, 1000), (3, 1000), (4, 1000), (8, 1000), (24, 1000), (32, 1000), (200, 1000))]
+    for (a, b), (share, same) in zip(pairs, rule(pairs)):
+        common = _bytes(*a) & _bytes(*b)
+        assert share or not common, (a, b)
+        if same:
+            assert _bytes(*a) == _bytes(*b), (a, b)
+    apart = [((1000, 1, 0, 9, 32, 16), (1016, 1, 0, 9, 32, 16)),           # halves of rows
+             ((1016, 1, 0, 9, 32, 16), (1000, 1, 0, 4, 32, 16)),
+             ((1000, 4, 320, 5, 32, 12), (1012, 4, 640, 5, 32, 20)),       # of a stack's rows
+             ((1000, 4, 320, 10, 16, 16), (1160, 4, 320, 10, 16, 16)),     # matrices by turns
+             ((1000, 4, 64, 1, 7, 32), (1032, 4, 64, 1, 9, 32)),
+             ((1000, 1, 0, 2, 50, 50), (1100, 1, 0, 2, 60, 50))]
+    assert all(r == (0, 0) for r in rule(apart))
+    one = (1000, 1, 5, 1, 99, 16)
+    assert rule([(one, (1000, 1, 7, 1, 16, 16))]) == [(1, 1)]
