@@ -409,8 +409,9 @@ nf_status nf_orthogonalize(const void* d_x, int32_t dtype, int64_t count, int64_
  *   M' = momentum M + G,  U = G + momentum M' (nesterov = 1) or M' (0),
  *   W' = (1 - eta decay) W - eta sqrt(max(1, rows / cols)) orthogonalised(U).
  * w_dtype, g_dtype: NF_F32 or NF_BF16 (not bf16 weights with fp32 gradients); the
- * momentum is fp32.  The orthogonalisation is w_dtype's.  d_w_out may be d_w and
- * d_m_out may be d_m; no other arrays may share bytes with d_m_out.
+ * momentum is fp32.  The orthogonalisation is w_dtype's.  d_w_out may be d_w, or
+ * d_g of the same type, and d_m_out may be d_m; no other arrays may share bytes
+ * with d_m_out, or d_g with d_w_out.
  * d_work: nf_orthogonalize_work(w_dtype, count, rows, cols) bytes, aligned to 256. */
 nf_status nf_muon_step(const void* d_w, int32_t w_dtype, const float* d_m, const void* d_g,
                        int32_t g_dtype, int64_t count, int64_t rows, int64_t cols, float eta,

@@ -753,6 +753,9 @@ nf_status nf_muon_step(const void* d_w, int32_t w_dtype, const float* d_m, const
       op_overlap(d_w, all * op_size(w_dtype), d_m_out, all * 4) ||
       op_overlap(d_w_out, all * op_size(w_dtype), d_m_out, all * 4))
     return op_fail(NF_EINVAL, "the new momentum overlaps weights or gradient");
+  // gradients of at most ORTH_SMALL rows or columns are read again while weights are written
+  if (op_overlap(d_g, all * op_size(g_dtype), d_w_out, all * op_size(w_dtype)) && !(d_g == d_w_out && g_dtype == w_dtype))
+    return op_fail(NF_EINVAL, "the new weights overlap the gradient without being it");
   OrthCall c{};
   c.count = count;
   c.rows = rows;

@@ -53,3 +53,17 @@ def test_orthogonalize_refuses_a_result_over_its_matrices(rows, cols):
             nf.nf_orthogonalize(x, out)
     torch.cuda.synchronize()
     assert torch.equal(buf, before)
+
+
+@pytest.mark.parametrize("rows,cols", [(40, 70), (70, 130)])
+def test_muon_step_in_the_gradients_place(rows, cols):
+    torch, nf = torch_cuda(), _nf()
+    note(f"muon in the gradient's place, {rows}x{cols}")
+    w, m, g = (_rand(rows, cols, seed=k) for k in range(3))
+    w_out, m_out = torch.empty_like(w), torch.empty_like(m)
+    nf.nf_muon_step(w, m, g, w_out, m_out, 0.1)
+    with pytest.raises(nf.NfError):
+        nf.nf_muon_step(w, m, g.view(torch.bfloat16).view(-1)[:rows * cols].view(rows, cols), g, m, 0.1)
+    nf.nf_muon_step(w, m, g, g, m, 0.1)
+    torch.cuda.synchronize()
+    assert torch.equal(g, w_out) and torch.equal(m, m_out)

@@ -10,7 +10,7 @@ import pytest
 
 from paper_1902_06714_amd import build, nf
 
-from .test_operators_cpu import E, ORTH, P, _call
+from .test_operators_cpu import E, MUON, ORTH, P, _call
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -28,6 +28,15 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 def test_orthogonalize_refuses_a_result_over_its_matrices(change):
     assert _call("nf_orthogonalize", ORTH, change) == E, nf.nf_last_error()
     assert "overlaps" in nf.nf_last_error()
+
+
+# new weights shifted on the gradient, or in its place with fp32 for bf16
+@pytest.mark.parametrize("change", [
+    {"wo": 3 * P + 4}, {"wo": 3 * P - 32}, {"wo": 3 * P, "gd": nf.NF_BF16}, {"wo": 3 * P - 128, "gd": nf.NF_BF16},
+    {"wo": 3 * P + 400, "rows": 100, "cols": 120}])
+def test_muon_step_refuses_new_weights_over_the_gradient(change):
+    assert _call("nf_muon_step", MUON, change) == E, nf.nf_last_error()
+    assert "gradient" in nf.nf_last_error()
 
 
 RULE = r"""
