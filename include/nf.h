@@ -330,7 +330,9 @@ nf_status nf_calib_mfma(int32_t dtype, int64_t iters, void* d_sink, void* stream
  * they may be captured in a HIP graph, and calls that share no arrays may run
  * on several streams and threads at once.  Arrays are row-major, `ld` elements
  * from row to row (columns <= ld; what lies between is neither read nor
- * written), aligned to their elements.  Sums are held in fp32 or more. */
+ * written), aligned to their elements.  Unless it is said otherwise, outputs and
+ * workspaces share no bytes with one another or with inputs.  Sums are held in
+ * fp32 or more. */
 
 /* Log probabilities, entropies and alternatives of rows of logits.
  * With z = scale x (scale > 0: one over a temperature), m = max z and

@@ -22,6 +22,8 @@
 // logits of some spread): the lanes whose own maximum is that large put them into LDS,
 // and each counts the larger ones.  More than fit there (rows of equal values)
 // are found by n_top searches for the next largest instead.
+#include <initializer_list>
+
 #include "ops_common.h"
 
 namespace nf {
@@ -750,6 +752,17 @@ nf_status check_gradient(const void* x, int64_t ld, const void* dx, int64_t ld_d
   return NF_OK;
 }
 
+// A row's results are written while others' inputs are read: no output shares bytes with the
+// targets, weights or statistics.  (The gradient and the logits: check_gradient.)
+nf_status check_apart(std::initializer_list<OpArray> out, std::initializer_list<OpArray> in) {
+  for (const OpArray& a : out)
+    for (const OpArray& b : in)
+      if (op_overlap(a.p, a.span(), b.p, b.span()) && op_share(a, b))
+        return op_fail(NF_EINVAL, "an output overlaps the logits, targets, weights or statistics");
+  return NF_OK;
+}
+OpArray column(const void* p, int64_t rows, int64_t bytes) { return {p, 1, 0, 1, 0, rows * bytes}; }
+
 // The workspace may be left out: rows then stay whole.
 nf_status check_logp_work(const void* work, int64_t have, const LogpPlan& p) {
   if (!work || !p.slices) return NF_OK;
@@ -806,8 +819,13 @@ nf_status nf_logprobs(const void* d_logits, int32_t dtype, int64_t rows, int64_t
   if (n_top > 0 && !d_top_ids && !d_top_logp) return op_fail(NF_EINVAL, "alternatives without a place for them");
   if (rows == 0) return NF_OK;
   const LogpPlan plan = logp_plan(op_size(dtype), rows, classes, n_top, false);
-  const nf_status ws = check_logp_work(d_work, work_bytes, plan);
-  if (ws != NF_OK) return ws;
+  nf_status more = check_logp_work(d_work, work_bytes, plan);
+  if (more != NF_OK) return more;
+  const int64_t size = op_size(dtype);
+  more = check_apart({column(d_logp, rows, 4), column(d_entropy, rows, 4), column(d_stat, rows, 8),
+                      column(d_top_ids, rows, 4 * n_top), column(d_top_logp, rows, 4 * n_top)},
+                     {{d_logits, 1, 0, rows, ld * size, classes * size}, column(d_targets, rows, 8)});
+  if (more != NF_OK) return more;
   const int units = op_compute_units();
   if (units <= 0) return op_fail(NF_EDEVICE, "no usable HIP device");
   return with_type(dtype, [&](auto e) {
@@ -845,6 +863,13 @@ nf_status nf_logprobs_train(const void* d_logits, int32_t dtype, int64_t rows, i
   if (st != NF_OK) return st;
   const LogpPlan plan = logp_plan(op_size(dtype), rows, classes, 0, true);
   st = check_logp_work(d_work, work_bytes, plan);
+  if (st != NF_OK) return st;
+  const int64_t size = op_size(dtype);
+  const OpArray targets = column(d_targets, rows, 8), g = column(d_g_logp, rows, 4), h = column(d_g_entropy, rows, 4);
+  const OpArray sums[] = {column(d_logp, rows, 4), column(d_entropy, rows, 4), column(d_stat, rows, 8)};
+  st = check_apart({sums[0], sums[1], sums[2]}, {{d_logits, 1, 0, rows, ld * size, classes * size}, targets, g, h});
+  if (st == NF_OK)
+    st = check_apart({{d_dlogits, 1, 0, rows, ld_d * size, classes * size}}, {targets, g, h, sums[0], sums[1], sums[2]});
   if (st != NF_OK) return st;
   const int units = op_compute_units();
   if (units <= 0) return op_fail(NF_EDEVICE, "no usable HIP device");
@@ -901,6 +926,11 @@ nf_status nf_logprobs_grad(const void* d_logits, int32_t dtype, int64_t rows, in
   if (d_g_logp && !d_targets) return op_fail(NF_EINVAL, "weights of log probabilities without targets");
   if (d_g_entropy && !d_entropy) return op_fail(NF_EINVAL, "weights of entropies without the entropies");
   st = check_gradient(d_logits, ld, d_dlogits, ld_d, dtype, rows, classes);
+  if (st != NF_OK) return st;
+  const int64_t size = op_size(dtype);
+  st = check_apart({{d_dlogits, 1, 0, rows, ld_d * size, classes * size}},
+                   {column(d_targets, rows, 8), column(d_stat, rows, 8), column(d_entropy, rows, 4),
+                    column(d_g_logp, rows, 4), column(d_g_entropy, rows, 4)});
   if (st != NF_OK) return st;
   const int units = op_compute_units();
   if (units <= 0) return op_fail(NF_EDEVICE, "no usable HIP device");

@@ -162,6 +162,9 @@ inline bool op_share(const OpArray& x, const OpArray& y) {
   };
   if (a.stride > 0 && a.stride == b.stride && by_turns(apart, a.stride, a.matrix(), b.matrix())) return false;
   if (a.even() && b.even() && a.pitch == b.pitch && by_turns(apart, a.pitch, a.width, b.width)) return false;
+  // one that lies between two rows of the other
+  if (a.even() && by_turns(apart, a.pitch, a.width, b.span())) return false;
+  if (b.even() && by_turns(-apart, b.pitch, b.width, a.span())) return false;
   return true;
 }
 // Whether they are the same array.

@@ -10,7 +10,7 @@ import pytest
 
 from paper_1902_06714_amd import build, nf
 
-from .test_operators_cpu import E, MUON, ORTH, P, _call
+from .test_operators_cpu import E, GRAD, LOGP, MUON, ORTH, P, TRAIN, _call
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -37,6 +37,23 @@ def test_orthogonalize_refuses_a_result_over_its_matrices(change):
 def test_muon_step_refuses_new_weights_over_the_gradient(change):
     assert _call("nf_muon_step", MUON, change) == E, nf.nf_last_error()
     assert "gradient" in nf.nf_last_error()
+
+
+# each array of a call on its own, a megabyte from the next
+APART = {name: {k: (i + 1) * P for i, k in enumerate(k for k in base if base[k] in (P, 2 * P))}
+         for name, base in (("nf_logprobs", LOGP), ("nf_logprobs_train", TRAIN), ("nf_logprobs_grad", GRAD))}
+
+
+@pytest.mark.parametrize("name,base,out,inputs", [
+    ("nf_logprobs", LOGP, ("logp", "ent", "stat", "ids", "alt"), ("x", "t")),
+    ("nf_logprobs_train", TRAIN, ("logp", "ent", "stat"), ("x", "t", "g", "h")),
+    ("nf_logprobs_train", TRAIN, ("dx",), ("t", "g", "h", "logp", "ent", "stat")),
+    ("nf_logprobs_grad", GRAD, ("dx",), ("t", "stat", "ent", "g", "h"))])
+def test_logprobs_refuse_outputs_over_their_inputs(name, base, out, inputs):
+    apart = APART[name]
+    for o, i in itertools.product(out, inputs):
+        assert _call(name, base, {**apart, o: apart[i] + 8}) == E, (o, i, nf.nf_last_error())
+        assert "overlaps" in nf.nf_last_error(), (o, i)
 
 
 RULE = r"""
@@ -92,6 +109,8 @@ def test_arrays_that_share_bytes_are_found(rule):
              ((1000, 4, 320, 5, 32, 12), (1012, 4, 640, 5, 32, 20)),       # of a stack's rows
              ((1000, 4, 320, 10, 16, 16), (1160, 4, 320, 10, 16, 16)),     # matrices by turns
              ((1000, 4, 64, 1, 7, 32), (1032, 4, 64, 1, 9, 32)),
+             ((1000, 1, 0, 9, 100, 20), (1020, 1, 0, 1, 0, 80)),           # between two rows
+             ((1340, 1, 0, 2, 8, 4), (1000, 2, 500, 5, 100, 40)),
              ((1000, 1, 0, 2, 50, 50), (1100, 1, 0, 2, 60, 50))]
     assert all(r == (0, 0) for r in rule(apart))
     one = (1000, 1, 5, 1, 99, 16)
