@@ -484,7 +484,7 @@ nf_status nf_quantize_rows(const void* d_x, int32_t dtype, int64_t rows, int64_t
   if (!d_x || !d_q || !d_scale) return op_fail(NF_EINVAL, "NULL pointer");
   if (!op_aligned(d_x, (uintptr_t)op_size(dtype)) || !op_aligned(d_q, 16))
     return op_fail(NF_EINVAL, "rows must be aligned to their elements, quantised rows to 16 bytes");
-  if (op_overlap(d_x, ((rows - 1) * ld + cols) * op_size(dtype), d_q, (rows - 1) * ld_q + whole16(cols)))
+  if (op_share({d_x, 1, 0, rows, ld * op_size(dtype), cols * op_size(dtype)}, {d_q, 1, 0, rows, ld_q, whole16(cols)}))
     return op_fail(NF_EINVAL, "the quantised rows overlap the rows");
   if (op_compute_units() <= 0) return op_fail(NF_EDEVICE, "no usable HIP device");
   return with_type(dtype, [&](auto e) {
@@ -506,7 +506,8 @@ nf_status nf_linear_i8(const int8_t* d_xq, int64_t ld_x, const float* d_x_scale,
   if (rows == 0) return NF_OK;
   if (!d_xq || !d_x_scale) return op_fail(NF_EINVAL, "NULL rows or scales");
   if (!op_aligned(d_xq, 16)) return op_fail(NF_EINVAL, "the rows are not aligned to 16 bytes");
-  if (op_overlap(d_xq, (rows - 1) * ld_x + whole16(inputs), d_y, ((rows - 1) * ld_y + outputs) * op_size(y_dtype)))
+  const int64_t size = op_size(y_dtype);
+  if (op_share({d_xq, 1, 0, rows, ld_x, whole16(inputs)}, {d_y, 1, 0, rows, ld_y * size, outputs * size}))
     return op_fail(NF_EINVAL, "the result overlaps the rows");
   const int units = op_compute_units();
   if (units <= 0) return op_fail(NF_EDEVICE, "no usable HIP device");
@@ -536,8 +537,8 @@ nf_status nf_linear_i8_dynamic(const void* d_x, int32_t x_dtype, int64_t ld_x, c
   if (rows == 0) return NF_OK;
   if (!d_x) return op_fail(NF_EINVAL, "NULL rows");
   if (!op_aligned(d_x, (uintptr_t)op_size(x_dtype))) return op_fail(NF_EINVAL, "the rows are not aligned to their elements");
-  if (op_overlap(d_x, ((rows - 1) * ld_x + inputs) * op_size(x_dtype), d_y,
-                 ((rows - 1) * ld_y + outputs) * op_size(y_dtype)))
+  const int64_t x_size = op_size(x_dtype), y_size = op_size(y_dtype);
+  if (op_share({d_x, 1, 0, rows, ld_x * x_size, inputs * x_size}, {d_y, 1, 0, rows, ld_y * y_size, outputs * y_size}))
     return op_fail(NF_EINVAL, "the result overlaps the rows");
   if (!d_work || !op_aligned(d_work, 16)) return op_fail(NF_EINVAL, "the workspace is NULL or not aligned to 16 bytes");
   if (work_bytes < nf_linear_i8_work(rows, inputs))

@@ -746,8 +746,8 @@ nf_status check_gradient(const void* x, int64_t ld, const void* dx, int64_t ld_d
   if (ld_dx > INT64_MAX / 4 / rows) return op_fail(NF_ESHAPE, "rows times pitch does not fit");
   if (!op_aligned(dx, (uintptr_t)op_size(dtype))) return op_fail(NF_EINVAL, "the gradient is not aligned to its elements");
   const int64_t e = op_size(dtype);
-  if (!(x == dx && ld == ld_dx) &&
-      op_overlap(x, ((rows - 1) * ld + classes) * e, dx, ((rows - 1) * ld_dx + classes) * e))
+  const OpArray in{x, 1, 0, rows, ld * e, classes * e}, out{dx, 1, 0, rows, ld_dx * e, classes * e};
+  if (op_share(in, out) && !op_same(in, out))
     return op_fail(NF_EINVAL, "the gradient overlaps the logits without being them");
   return NF_OK;
 }

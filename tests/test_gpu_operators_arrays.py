@@ -67,3 +67,53 @@ def test_muon_step_in_the_gradients_place(rows, cols):
     nf.nf_muon_step(w, m, g, g, m, 0.1)
     torch.cuda.synchronize()
     assert torch.equal(g, w_out) and torch.equal(m, m_out)
+
+
+@pytest.mark.parametrize("rows,classes", [(9, 50), (300, 1000), (5, 9000)])
+def test_gradient_beside_the_logits(rows, classes):
+    torch, nf = torch_cuda(), _nf()
+    note(f"gradient beside the logits, {rows}x{classes}")
+    wide = torch.full((rows, 2 * classes + 3), 7.0, device="cuda")
+    x, dx = wide[:, :classes], wide[:, classes + 1:2 * classes + 1]
+    x.copy_(_rand(rows, classes))
+    t, g, want = torch.arange(rows, device="cuda") % classes, _rand(rows), torch.empty(rows, classes, device="cuda")
+    stat = torch.empty(rows, 2, device="cuda")
+    nf.nf_logprobs(x, t, stat=stat)
+    nf.nf_logprobs_train(x, t, g, None, want)
+    nf.nf_logprobs_train(x, t, g, None, dx)
+    torch.cuda.synchronize()
+    assert torch.equal(dx, want)
+    nf.nf_logprobs_grad(x, t, stat, None, g, None, want)
+    nf.nf_logprobs_grad(x, t, stat, None, g, None, dx)
+    torch.cuda.synchronize()
+    assert torch.equal(dx, want)
+    assert (wide[:, classes] == 7.0).all() and (wide[:, 2 * classes + 1:] == 7.0).all()
+
+
+@pytest.mark.parametrize("rows,inputs,outputs", [(1, 100, 20), (3, 64, 30), (12, 130, 40), (100, 77, 90)])
+def test_linear_layer_beside_its_inputs(rows, inputs, outputs):
+    """A layer's outputs appended to its inputs' rows, as where later layers read both."""
+    torch, nf = torch_cuda(), _nf()
+    note(f"linear beside its inputs, {rows}x{inputs}->{outputs}")
+    wide = torch.full((rows, inputs + outputs), 7.0, device="cuda")
+    x, y = wide[:, :inputs], wide[:, inputs:]
+    x.copy_(_rand(rows, inputs))
+    wq = torch.zeros((outputs, (inputs + 15) // 16 * 16), dtype=torch.int8, device="cuda")
+    ws = torch.empty(outputs, device="cuda")
+    nf.nf_quantize_rows(_rand(outputs, inputs, seed=2), wq, ws)
+    want = torch.empty(rows, outputs, device="cuda")
+    nf.nf_linear_i8_dynamic(x.clone(), wq, ws, want, act="tanh")
+    nf.nf_linear_i8_dynamic(x, wq, ws, y, act="tanh")
+    torch.cuda.synchronize()
+    assert torch.equal(y, want)
+    with pytest.raises(nf.NfError):
+        nf.nf_linear_i8_dynamic(x, wq, ws, wide[:, inputs - 1:-1])
+    q = torch.full((rows, 256), 9, dtype=torch.int8, device="cuda")       # quantised rows beside the rows
+    q4 = q.view(torch.float32)
+    n = min(inputs, 32)
+    q4[:, :n].copy_(x[:, :n])
+    scale, want_q = torch.empty(rows, device="cuda"), torch.empty((rows, 32), dtype=torch.int8, device="cuda")
+    nf.nf_quantize_rows(q4[:, :n], q[:, 128:160], scale)
+    nf.nf_quantize_rows(x[:, :n], want_q, scale)
+    torch.cuda.synchronize()
+    assert torch.equal(q[:, 128:160], want_q) and (q[:, 160:] == 9).all()
