@@ -801,7 +801,8 @@ extern "C" {
 
 int64_t nf_logprobs_work(int32_t dtype, int64_t rows, int64_t classes, int32_t n_top, int32_t gradient) {
   op_begin();
-  if (!op_float_type(dtype) || rows < 0 || classes < 1 || n_top < 0 || n_top > NF_TOP_MAX || classes > (1 << 30)) {
+  if (!op_float_type(dtype) || rows < 0 || rows > 0x7fffffff || classes < 1 || classes > (1 << 30) || n_top < 0 ||
+      n_top > NF_TOP_MAX || (!gradient && n_top > classes)) {
     op_fail(NF_EINVAL, "sizes or type that the call would refuse");
     return -1;
   }

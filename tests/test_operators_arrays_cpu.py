@@ -56,6 +56,17 @@ def test_logprobs_refuse_outputs_over_their_inputs(name, base, out, inputs):
         assert "overlaps" in nf.nf_last_error(), (o, i)
 
 
+def test_workspaces_of_sizes_that_are_refused():
+    lib = nf.raw()
+    for rows, classes, top in ((1 << 31, 10, 0), (1 << 40, 131072, 5), (4, 6, 7), (0, 6, 7), (1, (1 << 30) + 1, 0)):
+        assert lib.nf_logprobs_work(nf.NF_F32, rows, classes, top, 0) == -1 and nf.nf_last_error() != ""
+        with pytest.raises(nf.NfError):
+            nf.nf_logprobs_work(nf.NF_F32, rows, classes, top)
+    assert lib.nf_logprobs_work(nf.NF_F32, 1 << 31, 10, 0, 1) == -1
+    assert lib.nf_logprobs_work(nf.NF_F32, (1 << 31) - 1, 10, 10, 0) == 0
+    assert lib.nf_logprobs_work(nf.NF_F32, 4, 6, 0, 1) == 0
+
+
 RULE = r"""
 #include <cstdio>
 #include "ops_common.h"
