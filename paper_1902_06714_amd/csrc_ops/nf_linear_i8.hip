@@ -132,19 +132,24 @@ __global__ void __launch_bounds__(THREADS) quant_kernel(const QuantArgs<T> a) {
 template <class T>
 hipError_t launch_quant(const T* x, int64_t ldx, int64_t rows, int cols, int8_t* q, int64_t ldq, float* scale,
                         hipStream_t s) {
-  const QuantArgs<T> a{x, ldx, ldq, rows, cols, (cols + 15) / 16 * 16, q, scale};
-  const int vecs = a.wide / Vec16<T>::N;
-#define NF_QUANT(TH, TPR, NV)     \
-  if (vecs <= (TPR) * (NV))       \
-    return op_launch(quant_kernel<T, TH, TPR, NV>, dim3((unsigned)((rows + (TH) / (TPR) - 1) / ((TH) / (TPR)))), \
-                    dim3(TH), s, a);
+  const int wide = (cols + 15) / 16 * 16, vecs = wide / Vec16<T>::N;
+  auto go = [&](auto threads, auto of_row, auto held) {
+    constexpr int TH = decltype(threads)::value, TPR = decltype(of_row)::value, NV = decltype(held)::value;
+    return op_each_launch(rows, TH, TH / TPR, 1, [&](int64_t first, int64_t n) {
+      const QuantArgs<T> b{x + first * ldx, ldx, ldq, n, cols, wide, q + first * ldq, scale + first};
+      return op_launch(quant_kernel<T, TH, TPR, NV>, dim3((unsigned)((n + TH / TPR - 1) / (TH / TPR))), dim3(TH), s, b);
+    });
+  };
+#define NF_QUANT(TH, TPR, NV) \
+  if (vecs <= (TPR) * (NV))   \
+    return go(std::integral_constant<int, TH>(), std::integral_constant<int, TPR>(), std::integral_constant<int, NV>());
   NF_QUANT(256, 16, 2)
   NF_QUANT(256, 64, 1)
   NF_QUANT(256, 64, 4)
   NF_QUANT(256, 256, 2)
   NF_QUANT(256, 256, 8)
 #undef NF_QUANT
-  return op_launch(quant_kernel<T, 1024, 1024, 0>, dim3((unsigned)rows), dim3(1024), s, a);
+  return go(std::integral_constant<int, 1024>(), std::integral_constant<int, 1024>(), std::integral_constant<int, 0>());
 }
 
 // ---- the product ---------------------------------------------------------------
@@ -254,11 +259,20 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * G * 64, OCC) linear_ke
 
 template <class T, int BM, int WM, int WN, int NS, int G, int OCC, int BN = BM>
 hipError_t launch_linear_tile(LinearArgs a, hipStream_t s) {
-  a.mt = (a.rows + BM - 1) / BM;
+  constexpr int THREADS = (BM / WM) * (BN / WN) * G * 64;
   a.nt = (a.outputs + BN - 1) / BN;
-  a.total = a.mt * a.nt;
-  return op_launch(linear_kernel<T, BM, BN, WM, WN, NS, G, OCC>, dim3(mm_grid(a.total)),
-                  dim3((BM / WM) * (BN / WN) * G * 64), s, a);
+  const int64_t rows = a.rows;
+  return op_each_launch((rows + BM - 1) / BM, THREADS, 1, a.nt, [&](int64_t first, int64_t n) {
+    LinearArgs b = a;
+    const int64_t row = first * BM;
+    b.xq += row * a.ldx;
+    b.x_scale += row;
+    b.y = static_cast<T*>(a.y) + row * a.ldy;
+    b.rows = (int)(rows - row < n * BM ? rows - row : n * BM);
+    b.mt = (int)n;
+    b.total = b.mt * b.nt;
+    return op_launch(linear_kernel<T, BM, BN, WM, WN, NS, G, OCC>, dim3(mm_grid(b.total)), dim3(THREADS), s, b);
+  });
 }
 
 // ---- few rows: the weights' bytes ----------------------------------------------

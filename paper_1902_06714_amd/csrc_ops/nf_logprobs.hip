@@ -52,6 +52,22 @@ struct LogpArgs {
   int slices, slice;
   float4* part;                  // [rows][slices]: m, sum, sum of exp times d
   unsigned long long* keys;      // [rows][slices][n_top]
+
+  LogpArgs of_rows(int64_t first, int64_t n) const {       // (of whole rows)
+    LogpArgs a = *this;
+    a.rows = n;
+    a.x += first * ld;
+    if (target) a.target += first;
+    if (g) a.g += first;
+    if (h) a.h += first;
+    if (logp) a.logp += first;
+    if (entropy) a.entropy += first;
+    if (stat) a.stat += 2 * first;
+    if (top_ids) a.top_ids += first * n_top;
+    if (top_logp) a.top_logp += first * n_top;
+    if (dx) a.dx += first * ld_dx;
+    return a;
+  }
 };
 
 // NaN above all numbers, -0 as 0, and nothing at 0 but places that hold no value
@@ -574,6 +590,19 @@ struct GradArgs {
   const float* entropy;
   const float* g;
   const float* h;
+
+  GradArgs of_rows(int64_t first, int64_t n) const {
+    GradArgs a = *this;
+    a.rows = n;
+    a.x += first * ld;
+    a.dx += first * ld_dx;
+    if (target) a.target += first;
+    a.stat += 2 * first;
+    if (entropy) a.entropy += first;
+    if (g) a.g += first;
+    if (h) a.h += first;
+    return a;
+  }
 };
 
 constexpr int GRAD_VECS = 2;
@@ -669,12 +698,19 @@ hipError_t launch_parts(LogpArgs<T> a, const LogpPlan& p, char* work, hipStream_
 template <class T>
 hipError_t launch_grad(GradArgs<T> a, hipStream_t s) {
   constexpr int64_t per = Vec16<T>::N * GRAD_VECS;        // of a thread
-  auto blocks = [&](int64_t lanes) { return dim3((unsigned)((a.rows + 256 / lanes - 1) / (256 / lanes))); };
   a.per_row = (int)((a.classes + 256 * per - 1) / (256 * per));
-  if (a.classes <= 4 * per) return op_launch(logp_grad_kernel<T, 4>, blocks(4), dim3(256), s, a);
-  if (a.classes <= 16 * per) return op_launch(logp_grad_kernel<T, 16>, blocks(16), dim3(256), s, a);
-  if (a.classes <= 64 * per) return op_launch(logp_grad_kernel<T, 64>, blocks(64), dim3(256), s, a);
-  return op_launch(logp_grad_kernel<T, 256>, dim3((unsigned)(a.rows * a.per_row)), dim3(256), s, a);
+  auto go = [&](auto l) {
+    constexpr int L = decltype(l)::value;
+    const int64_t per_row = L == 256 ? a.per_row : 1;
+    return op_each_launch(a.rows, 256, 256 / L, per_row, [&](int64_t first, int64_t n) {
+      return op_launch(logp_grad_kernel<T, L>, dim3((unsigned)((n * per_row + 256 / L - 1) / (256 / L))), dim3(256), s,
+                       a.of_rows(first, n));
+    });
+  };
+  if (a.classes <= 4 * per) return go(std::integral_constant<int, 4>());
+  if (a.classes <= 16 * per) return go(std::integral_constant<int, 16>());
+  if (a.classes <= 64 * per) return go(std::integral_constant<int, 64>());
+  return go(std::integral_constant<int, 256>());
 }
 
 template <class T, bool GRAD>
@@ -683,8 +719,10 @@ hipError_t launch_logp(const LogpArgs<T>& a, int units, hipStream_t s) {
     const int half = (a.classes + 1) / 2;
     auto go = [&](auto g) {
       constexpr int G = decltype(g)::value;
-      const int64_t blocks = (a.rows + 256 / G - 1) / (256 / G);
-      return op_launch(logp_small_kernel<T, G, GRAD>, dim3((unsigned)blocks), dim3(256), s, a);
+      return op_each_launch(a.rows, 256, 256 / G, 1, [&](int64_t first, int64_t n) {
+        return op_launch(logp_small_kernel<T, G, GRAD>, dim3((unsigned)((n + 256 / G - 1) / (256 / G))), dim3(256), s,
+                         a.of_rows(first, n));
+      });
     };
     if (half <= 8) return go(std::integral_constant<int, 8>());
     if (half <= 16) return go(std::integral_constant<int, 16>());
@@ -702,8 +740,10 @@ hipError_t launch_logp(const LogpArgs<T>& a, int units, hipStream_t s) {
   //   1024 54, 1024 and 8 51; 1000 x 131072 bf16 by 512 177, by 1024 170.
   //   Few rows wait for one another's steps, so more threads: 1 x 32768 bf16, 1024 and 4 7.5, 512 and 8
   //   8.2; 20 x 50000 f32 by 1024 15, by 512 17.
-#define NF_ROW(TH, NV) \
-  return op_launch(logp_row_kernel<T, TH, NV, GRAD>, dim3((unsigned)a.rows), dim3(TH), s, a)
+#define NF_ROW(TH, NV)                                                                               \
+  return op_each_launch(a.rows, TH, 1, 1, [&](int64_t first, int64_t n) {                            \
+    return op_launch(logp_row_kernel<T, TH, NV, GRAD>, dim3((unsigned)n), dim3(TH), s, a.of_rows(first, n)); \
+  })
   const bool few = a.rows <= units;
   if (vecs <= 64) NF_ROW(64, 1);
   if (vecs <= 256) NF_ROW(64, 4);
@@ -950,7 +990,6 @@ nf_status nf_logprobs_grad(const void* d_logits, int32_t dtype, int64_t rows, in
     a.entropy = d_entropy;
     a.g = d_g_logp;
     a.h = d_g_entropy;
-    if (rows * ((classes + 255) / 256) > 0x7fffffff) return op_fail(NF_ESHAPE, "too many logits for one call");
     return op_result(launch_grad<T>(a, static_cast<hipStream_t>(stream)), "gradient of log probabilities");
   });
 }

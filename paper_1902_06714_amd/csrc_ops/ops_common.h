@@ -118,6 +118,19 @@ inline hipError_t op_launch(void (*kernel)(P...), dim3 grid, dim3 block, hipStre
   return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, argv, 0, s);
 }
 
+// Rows in as many launches as they take: f(first, n) launches rows first .. first + n - 1 in
+// workgroups of `block` threads, `per_block` rows each or `per_row` to a row.  (A grid
+// holds fewer than 2^32 threads, and a grid of tiles up to 7 workgroups more.)
+template <class F>
+hipError_t op_each_launch(int64_t rows, int64_t block, int64_t per_block, int64_t per_row, F&& f) {
+  const int64_t most = (0xffffffffll / block - 7) / per_row * per_block;
+  for (int64_t first = 0; first < rows; first += most) {
+    const hipError_t e = f(first, rows - first < most ? rows - first : most);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 // Compute units of the current device, or 0 where there is none (asked once
 // for each device).
 int op_compute_units();

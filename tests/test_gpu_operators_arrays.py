@@ -117,3 +117,56 @@ def test_linear_layer_beside_its_inputs(rows, inputs, outputs):
     nf.nf_quantize_rows(x[:, :n], want_q, scale)
     torch.cuda.synchronize()
     assert torch.equal(q[:, 128:160], want_q) and (q[:, 160:] == 9).all()
+
+
+# more rows than one grid holds threads for: up to 128 classes four rows share a
+# workgroup of 256, longer ones have a wave each
+@pytest.mark.parametrize("classes", [65, 129])
+def test_log_probabilities_of_more_rows_than_a_grid_holds(classes):
+    torch, nf = torch_cuda(), _nf()
+    rows = (1 << 26) + 9
+    note(f"log probabilities of {rows} rows of {classes}")
+    x = _rand_rows(rows, classes)
+    t = torch.randint(0, classes, (rows,), device="cuda")
+    g = torch.full((rows,), 0.5, device="cuda")
+    logp, ids = torch.full((rows,), 1.0, device="cuda"), torch.full((rows, 1), -1, dtype=torch.int32, device="cuda")
+    stat = torch.empty((rows, 2), device="cuda")
+    nf.nf_logprobs(x, t, logp=logp, stat=stat, top_ids=ids)
+    assert (logp <= 0).all() and (ids >= 0).all()
+    parts = [slice(0, 100), slice((1 << 26) - 40, (1 << 26) - 10), slice(rows - 50, rows)]
+    held = [x[p].clone() for p in parts]
+    for p, a in zip(parts, held):
+        l2, i2 = torch.empty_like(logp[p]), torch.empty_like(ids[p])
+        nf.nf_logprobs(a, t[p], logp=l2, top_ids=i2)
+        assert torch.equal(l2, logp[p]) and torch.equal(i2, ids[p])
+    nf.nf_logprobs_train(x, t, g, None, x)
+    for p, a in zip(parts, held):
+        nf.nf_logprobs_train(a, t[p], g[p], None, a)
+        assert torch.equal(a, x[p])
+
+
+def test_gradient_of_more_rows_than_a_grid_holds():
+    torch, nf = torch_cuda(), _nf()
+    rows, classes = (1 << 24) + 9, 1025                  # 256 threads a row
+    note(f"gradient of {rows} rows of {classes}")
+    x = _rand_rows(rows, classes)
+    t, g = torch.randint(0, classes, (rows,), device="cuda"), torch.full((rows,), 0.5, device="cuda")
+    stat = torch.empty((rows, 2), device="cuda")
+    nf.nf_logprobs(x, stat=stat)
+    parts = [slice(0, 100), slice((1 << 24) - 40, (1 << 24) + 1), slice(rows - 5, rows)]
+    held = [x[p].clone() for p in parts]
+    nf.nf_logprobs_grad(x, t, stat, None, g, None, x)
+    for p, a in zip(parts, held):
+        nf.nf_logprobs_grad(a, t[p], stat[p], None, g[p], None, a)
+        assert torch.equal(a, x[p])
+
+
+def _rand_rows(rows, classes):
+    """bf16 rows that differ from one another, few of them drawn."""
+    torch = torch_cuda()
+    x = torch.empty((rows, classes), dtype=torch.bfloat16, device="cuda")
+    some = _rand(4099, classes).to(torch.bfloat16)
+    for r in range(0, rows, 4099 * 1024):
+        n = min(rows - r, 4099 * 1024)
+        x[r:r + n].copy_(some.repeat((n + 4098) // 4099, 1)[:n])
+    return x

@@ -89,18 +89,23 @@ def _bytes(p, count, stride, rows, pitch, width):
     return {p + k * stride + r * pitch + c for k in range(count) for r in range(rows) for c in range(width)}
 
 
-@pytest.fixture(scope="module")
-def rule(tmp_path_factory):
-    d = tmp_path_factory.mktemp("rule")
-    (d / "rule.hip").write_text(RULE)
+def _program(d, text):
+    """A host program of the operators' sources: lines of numbers in, lines of numbers out."""
+    (d / "rule.hip").write_text(text)
     subprocess.run([build.hipcc(), "--offload-arch=gfx950", "-O1", "-std=c++17", "-I", os.path.join(ROOT, "include"),
                     "-I", build.CSRC, "-I", build.OPS, str(d / "rule.hip"), "-o", str(d / "rule")], check=True)
 
-    def ask(pairs):
-        text = "\n".join(" ".join(str(v) for v in a + b) for a, b in pairs)
+    def ask(lines):
+        text = "\n".join(" ".join(str(v) for v in line) for line in lines)
         out = subprocess.run([str(d / "rule")], input=text, capture_output=True, text=True, check=True).stdout
         return [tuple(map(int, line.split())) for line in out.splitlines()]
     return ask
+
+
+@pytest.fixture(scope="module")
+def rule(tmp_path_factory):
+    ask = _program(tmp_path_factory.mktemp("rule"), RULE)
+    return lambda pairs: ask([a + b for a, b in pairs])
 
 
 def test_arrays_that_share_bytes_are_found(rule):
@@ -126,3 +131,37 @@ def test_arrays_that_share_bytes_are_found(rule):
     assert all(r == (0, 0) for r in rule(apart))
     one = (1000, 1, 5, 1, 99, 16)
     assert rule([(one, (1000, 1, 7, 1, 16, 16))]) == [(1, 1)]
+
+
+LAUNCHES = r"""
+#include <cstdio>
+#include "ops_common.h"
+int main() {
+  long long rows, block, per_block, per_row;
+  while (std::scanf("%lld %lld %lld %lld", &rows, &block, &per_block, &per_row) == 4) {
+    long long next = 0, launches = 0, most = 0;
+    const hipError_t e = nf::op_each_launch(rows, block, per_block, per_row, [&](int64_t first, int64_t n) {
+      if (first != next || n < 1) return hipErrorInvalidValue;
+      next += n;
+      ++launches;
+      const long long threads = ((n * per_row + per_block - 1) / per_block + 7) / 8 * 8 * block;
+      if (threads > most) most = threads;
+      return hipSuccess;
+    });
+    std::printf("%d %lld %lld %d\n", (int)(e == hipSuccess), next, launches, (int)(most < (1ll << 32)));
+  }
+}
+"""
+
+
+def test_rows_past_a_grid_take_several_launches(tmp_path):
+    """Rows up to 2^31 - 1 by every kernel's workgroups: whole, in order, each grid below
+    2^32 threads, and one launch where one holds them."""
+    ways = [(256, 32, 1), (256, 4, 1), (64, 1, 1), (256, 1, 1), (512, 1, 1), (1024, 1, 1), (256, 1, 3), (256, 1, 1 << 19),
+            (512, 1, 1024)]
+    asked = [(rows, *w) for rows in (1, 1000, (1 << 22) - 8, 1 << 22, 1 << 24, (1 << 26) + 9, (1 << 31) - 1) for w in ways]
+    for (rows, block, per_block, per_row), got in zip(asked, _program(tmp_path, LAUNCHES)(asked)):
+        assert got[0] == 1 and got[1] == rows and got[3] == 1, (rows, block, per_block, per_row, got)
+        blocks = (rows * per_row + per_block - 1) // per_block
+        if (blocks + 8 * per_row) * block < 1 << 32:
+            assert got[2] == 1, (rows, block, per_block, per_row, got)
