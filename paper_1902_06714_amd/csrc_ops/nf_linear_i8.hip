@@ -431,18 +431,12 @@ bool few_quantises(int64_t rows, int64_t inputs) {
 
 template <class T>
 hipError_t launch_linear_as(const LinearArgs& a, int units, hipStream_t s) {
-  auto tiles = [&](int64_t b) { return ((a.rows + b - 1) / b) * ((a.outputs + b - 1) / b); };
-  switch (mm_shape(tiles, units, (a.bytes + MM_STAGE - 1) / MM_STAGE)) {
+  switch (linear_shape(a.rows, a.outputs, a.bytes, units)) {
     case MM_32_GROUPS: return launch_linear_tile<T, 32, 32, 32, 3, 4, 1>(a, s);
     case MM_64_GROUPS: return launch_linear_tile<T, 64, 32, 32, 3, 2, 2>(a, s);
     case MM_64: return launch_linear_tile<T, 64, 32, 32, 3, 1, 3>(a, s);
-    case MM_128:
-      // 128 x 192 where all tiles run at once then, two on a compute unit (us, 128 and 192 columns: 784
-      // inputs 10000 x 1024 f32 25.3, 23.2, bf16 25.8, 24.8; 300, 16000 x 600 21.6, 21.2; 100, 14000 x 700
-      // 20.2, 19.7)
-      if (tiles(128) > 2 * units && ((a.rows + 127) / 128) * ((a.outputs + 191) / 192) <= 2 * units)
-        return launch_linear_tile<T, 128, 64, 96, 2, 1, 2, 192>(a, s);
-      return launch_linear_tile<T, 128, 64, 32, 2, 1, 4>(a, s);
+    case MM_128: return launch_linear_tile<T, 128, 64, 32, 2, 1, 4>(a, s);
+    case MM_128_192: return launch_linear_tile<T, 128, 64, 96, 2, 1, 2, 192>(a, s);
     case MM_192: return launch_linear_tile<T, 192, 96, 96, 3, 1, 1>(a, s);
     default: return launch_linear_tile<T, 256, 128, 64, 2, 1, 2>(a, s);
   }

@@ -79,8 +79,8 @@ OrthPlan orth_plan(bool parts, int64_t rows, int64_t cols) {
   OrthPlan p{};
   p.m = (int)(rows < cols ? rows : cols);
   p.n = (int)(rows < cols ? cols : rows);
-  p.kx = (int)up((int64_t)p.n * (parts ? 4 : 2), 128);
-  p.kt = (int)up((int64_t)p.m * (parts ? 4 : 2), parts ? 128 : 64);
+  p.kx = (int)orth_wide(parts, p.n);
+  p.kt = (int)orth_narrow(parts, p.m);
   p.px = odd_pitch(p.kx);
   p.pt = odd_pitch(p.kt);
   p.pm = parts ? 0 : odd_pitch(2 * (int64_t)p.kx);
@@ -240,8 +240,6 @@ __global__ void __launch_bounds__(256) orth_fill_kernel(const FillArgs<T> a) {
 }
 
 // ---- the products -------------------------------------------------------------
-enum OrthProduct { PROD_GRAM, PROD_POLY, PROD_STEP, PROD_LAST };
-
 struct MmArgs {
   OrthPlan p;
   char* work;
@@ -507,13 +505,7 @@ hipError_t launch_tile(MmArgs a, int64_t count, hipStream_t s) {
 
 template <int KIND, int PROD>
 hipError_t launch_product(const MmArgs& a, int64_t count, int units, hipStream_t s) {
-  constexpr bool SQUARE = PROD == PROD_GRAM || PROD == PROD_POLY;
-  auto tiles = [&](int64_t b) {
-    const int64_t m = (a.p.m + b - 1) / b, n = (a.p.n + b - 1) / b;
-    return count * (SQUARE ? m * (m + 1) / 2 : m * n);
-  };
-  const int64_t bytes = PROD == PROD_GRAM ? a.p.kx : a.p.kt;
-  switch (mm_shape(tiles, units, (bytes + MM_STAGE - 1) / MM_STAGE)) {
+  switch (orth_shape((OrthProduct)PROD, KIND == MM_PARTS2, count, a.p.m, a.p.n, units)) {
     case MM_32_GROUPS: return launch_tile<KIND, PROD, 32, 32, 32, 3, 4, 1>(a, count, s);
     case MM_64_GROUPS: return launch_tile<KIND, PROD, 64, 32, 32, 3, 2, 2>(a, count, s);
     case MM_64: return launch_tile<KIND, PROD, 64, 32, 32, 3, 1, 3>(a, count, s);

@@ -1,0 +1,145 @@
+"""The operators' matrix products in every tile they have, past its edges, with what lies
+around the results left alone.
+
+Tolerances are those of test_gpu_operators, of the result's norm, and so that no single
+element is off: errors of that norm spread over the elements are within 8 of their root
+mean square in each.  A step's weights: fp32 2 u of themselves more, bf16 ut."""
+
+import numpy as np
+import pytest
+
+from oracle import operators as ref
+
+from .gpu_run import note, torch_cuda
+from .operator_sizes import LINEAR, MUON, ORTH
+
+pytestmark = pytest.mark.gpu
+
+TOL = {"f32": 2e-5, "bf16": 6e-3}
+U_OF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+
+
+def _nf():
+    from paper_1902_06714_amd import nf
+    return nf
+
+
+def _dt(name):
+    torch = torch_cuda()
+    return {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[name]
+
+
+def _rand(shape, dtype, seed):
+    torch = torch_cuda()
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    return torch.randn(shape, generator=gen, device="cuda").to(_dt(dtype))
+
+
+class Framed:
+    """A GPU array of matrices whose rows lie `pad` apart, in an allocation that holds 7
+    wherever the array does not."""
+
+    def __init__(self, shape, dtype, pad, ahead=1):
+        torch = torch_cuda()
+        *count, rows, cols = shape
+        n = int(np.prod(count, dtype=np.int64)) if count else 1
+        self.flat = torch.full((ahead + n * rows * (cols + pad) + 64,), 7.0, device="cuda").to(_dt(dtype))
+        body = self.flat[ahead:ahead + n * rows * (cols + pad)]
+        self.view = body.view(*count, rows, cols + pad)[..., :cols]
+        self.inside = torch.zeros_like(self.flat, dtype=torch.bool)
+        self.inside[ahead:ahead + n * rows * (cols + pad)].view(*count, rows, cols + pad)[..., :cols] = True
+
+    def check(self):
+        assert (self.flat[~self.inside] == 7.0).all(), "written past the array"
+
+
+def _orthogonalised(u):
+    torch = torch_cuda()
+    u = u.double()
+    u = u / torch.linalg.matrix_norm(u, keepdim=True)
+    turned = u.shape[-2] > u.shape[-1]
+    u = u.transpose(1, 2).contiguous() if turned else u
+    a, b, c = ref.QUINTIC
+    for _ in range(ref.STEPS):
+        gram = torch.matmul(u, u.transpose(1, 2).contiguous())
+        u = a * u + torch.matmul(b * gram + c * torch.matmul(gram, gram), u)
+    return u.transpose(1, 2) if turned else u
+
+
+def _held(got, want, tol, size, what):
+    """size: of an element's own rounding"""
+    torch = torch_cuda()
+    off = (got.double() - want).abs()
+    norm = torch.linalg.matrix_norm(want)
+    over = torch.linalg.matrix_norm(torch.clamp_min(off - size, 0.0)) / norm
+    assert over.max().item() <= tol, f"{what}: {over.max().item():.3g} of the norm"
+    rms = norm / np.sqrt(want.shape[-2] * want.shape[-1])
+    part = (off / (8 * tol * rms[..., None, None] + size)).amax().item()
+    assert part <= 1.0, f"{what}: {part:.3g} of an element's tolerance"
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("turned", [False, True])
+@pytest.mark.parametrize("size", ORTH, ids=lambda s: "x".join(map(str, s)))
+def test_orthogonalize(size, turned, dtype):
+    torch, nf = torch_cuda(), _nf()
+    count, rows, cols = (size[0], size[2], size[1]) if turned else size
+    note(f"orthogonalize {count} x {rows} x {cols} {dtype}")
+    x = _rand((count, rows, cols), dtype, rows)
+    out = Framed((count, rows, cols), dtype, 3)
+    nf.nf_orthogonalize(x, out.view)
+    torch.cuda.synchronize()
+    out.check()
+    want = _orthogonalised(x)
+    _held(out.view, want, TOL[dtype], U_OF[dtype] * want.abs(), "orthogonalised")
+
+
+@pytest.mark.parametrize("w_dtype,g_dtype", [("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16")])
+@pytest.mark.parametrize("turned", [False, True])
+@pytest.mark.parametrize("size", MUON, ids=lambda s: "x".join(map(str, s)))
+def test_muon_step(size, turned, w_dtype, g_dtype):
+    torch, nf = torch_cuda(), _nf()
+    count, rows, cols = (size[0], size[2], size[1]) if turned else size
+    note(f"muon {count} x {rows} x {cols} {w_dtype} {g_dtype}")
+    shape = (count, rows, cols)
+    w, g, m = _rand(shape, w_dtype, 1), _rand(shape, g_dtype, 2), _rand(shape, "f32", 3)
+    wo, mo = Framed(shape, w_dtype, 0), Framed(shape, "f32", 0)
+    eta, mu, decay = (float(np.float32(v)) for v in (0.05, 0.9, 0.2))
+    nf.nf_muon_step(w, m, g, wo.view, mo.view, eta, mu, True, decay)
+    torch.cuda.synchronize()
+    wo.check()
+    mo.check()
+    m2 = mu * m.double() + g.double()
+    assert ((mo.view.double() - m2).abs() <= 4 * 2.0 ** -24 * (m2.abs() + g.double().abs())).all()
+    rate = eta * np.sqrt(max(1.0, rows / cols))
+    step = rate * _orthogonalised(g.double() + mu * m2)
+    # what the step did, with the weights' own rounding
+    want = w.double() * (1.0 - eta * decay)
+    size = 2 * 2.0 ** -24 * want.abs() + U_OF[w_dtype] * (want - step).abs()
+    _held(want - wo.view.double(), step, TOL[w_dtype], size, "update")
+
+
+@pytest.mark.parametrize("x_dtype,y_dtype", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f16"), ("bf16", "f32")])
+@pytest.mark.parametrize("size", LINEAR, ids=lambda s: "x".join(map(str, s)))
+def test_linear(size, x_dtype, y_dtype):
+    torch, nf = torch_cuda(), _nf()
+    rows, inputs, outputs = size
+    note(f"linear {rows} x {inputs} -> {outputs} {x_dtype} {y_dtype}")
+    x = _rand((rows, inputs), x_dtype, 5)
+    wide = (inputs + 15) // 16 * 16
+    wq = torch.zeros((outputs, wide), dtype=torch.int8, device="cuda")
+    wq[:, :inputs] = torch.randint(-128, 128, (outputs, inputs), device="cuda")
+    ws, b = torch.rand(outputs, device="cuda") / (20 * inputs ** 0.5), _rand((outputs,), "f32", 6)
+    y = Framed((rows, outputs), y_dtype, 5)
+    nf.nf_linear_i8_dynamic(x, wq, ws, y.view, bias=b, act="relu")
+    torch.cuda.synchronize()
+    y.check()
+    q, s = ref.quantize_rows(x.float().cpu().numpy())
+    z = torch.matmul(torch.as_tensor(q).cuda().double(), wq[:, :inputs].double().t().contiguous())     # (whole numbers: exact)
+    z = z * torch.as_tensor(s).cuda().double()[:, None] * ws.double()
+    want = torch.relu(z + b.double())
+    u = 2.0 ** -24
+    tol = 4 * u * (z.abs() + b.double().abs()) + (4 * u + U_OF[y_dtype]) * want + 2.0 ** -25
+    off = ((y.view.double() - want).abs() / tol).amax().item()
+    assert off <= 1.0, f"{off:.3g} of the tolerance"
