@@ -78,11 +78,20 @@ int elem_code(const at::Tensor& t) {
   }
 }
 
-// nf_dtype of a GPU tensor on the current device
-int elem(const at::Tensor& t, const char* name) {
+// The current device, asked once a call, which all of a call's tensors lie on.
+struct Device {
+  long at = -1;
+  void holds(const at::Tensor& t, const char* name) {
+    if (at < 0) at = current_device();
+    if (t.get_device() != at) refuse(PyExc_ValueError, "%s is not on the current device", name);
+  }
+};
+
+// nf_dtype of a tensor on the device
+int elem(Device& dev, const at::Tensor& t, const char* name) {
   const int code = elem_code(t);
   if (code < 0 || !t.is_cuda()) refuse(PyExc_ValueError, "%s must be an fp32, bf16 or fp16 GPU tensor", name);
-  if (t.get_device() != current_device()) refuse(PyExc_ValueError, "%s is not on the current device", name);
+  dev.holds(t, name);
   return code;
 }
 
@@ -103,21 +112,23 @@ Matrix matrix(const at::Tensor& t, const char* name, int64_t rows, int64_t cols)
     refuse(PyExc_ValueError, "%s must be 2-D of shape (%lld, %lld)", name, (long long)rows, (long long)cols);
   return matrix(t, name);
 }
-Matrix bytes_matrix(PyObject* o, const char* name) {
+Matrix bytes_matrix(Device& dev, PyObject* o, const char* name) {
   const at::Tensor& t = tensor(o, name);
   if (t.scalar_type() != at::kChar || !t.is_cuda()) refuse(PyExc_ValueError, "%s must be an int8 GPU tensor", name);
+  dev.holds(t, name);
   return matrix(t, name);
 }
 
 // pointer of a contiguous GPU tensor of this type and shape (of any with the sizes of
 // `like`), NULL for None
-void* whole(const at::Tensor& t, const char* name, at::ScalarType type, at::IntArrayRef shape) {
+void* whole(Device& dev, const at::Tensor& t, const char* name, at::ScalarType type, at::IntArrayRef shape) {
   if (t.scalar_type() != type || !t.is_cuda() || t.sizes() != shape || !t.is_contiguous())
     refuse(PyExc_ValueError, "%s must be a contiguous GPU tensor of the type and shape that go with the others", name);
+  dev.holds(t, name);
   return t.data_ptr();
 }
-void* vector(PyObject* o, const char* name, at::ScalarType type, at::IntArrayRef shape) {
-  return o == Py_None ? nullptr : whole(tensor(o, name), name, type, shape);
+void* vector(Device& dev, PyObject* o, const char* name, at::ScalarType type, at::IntArrayRef shape) {
+  return o == Py_None ? nullptr : whole(dev, tensor(o, name), name, type, shape);
 }
 
 // the caller's workspace, or one from torch's allocator, which hands it on only
@@ -126,7 +137,7 @@ struct Work {
   at::Tensor keep;
   void* p = nullptr;
   int64_t bytes = 0;
-  void take(PyObject* o, int64_t need, const at::Tensor& like) {
+  void take(Device& dev, PyObject* o, int64_t need, const at::Tensor& like) {
     if (o == Py_None) {
       if (need <= 0) return;
       Unlocked u;
@@ -134,6 +145,7 @@ struct Work {
     } else {
       keep = tensor(o, "work");
       if (!keep.is_cuda() || !keep.is_contiguous()) refuse(PyExc_ValueError, "work must be a contiguous GPU tensor");
+      dev.holds(keep, "work");
     }
     p = keep.data_ptr();
     bytes = keep.numel() * keep.element_size();
@@ -167,61 +179,64 @@ PyObject* guarded(Py_ssize_t have, Py_ssize_t want, F&& f) {
 // logits, targets, logp, entropy, stat, top_ids, top_logp, scale, work, stream
 PyObject* logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 10, [&] {
+    Device dev;
     const at::Tensor& x = tensor(a[0], "logits");
-    const int code = elem(x, "logits");
+    const int code = elem(dev, x, "logits");
     const Matrix m = matrix(x, "logits");
     int64_t top = 0;
     for (int k : {6, 5})
       if (a[k] != Py_None) top = tensor(a[k], "top").dim() ? THPVariable_Unpack(a[k]).size(-1) : 0;
     if (top > NF_TOP_MAX) top = NF_TOP_MAX + 1;            // refused below
     Work w;
-    w.take(a[8], nf_logprobs_work(code, m.rows, m.cols < 1 ? 1 : m.cols, (int)(top > NF_TOP_MAX ? 0 : top), 0), x);
+    w.take(dev, a[8], nf_logprobs_work(code, m.rows, m.cols < 1 ? 1 : m.cols, (int)(top > NF_TOP_MAX ? 0 : top), 0), x);
     return call(nf_logprobs, m.p, code, m.rows, m.cols, m.ld, (float)number(a[7]),
-                       (const int64_t*)vector(a[1], "targets", at::kLong, {m.rows}), (int)top,
-                       (float*)vector(a[2], "logp", at::kFloat, {m.rows}),
-                       (float*)vector(a[3], "entropy", at::kFloat, {m.rows}),
-                       (float*)vector(a[4], "stat", at::kFloat, {m.rows, 2}),
-                       (int32_t*)vector(a[5], "top_ids", at::kInt, {m.rows, top}),
-                       (float*)vector(a[6], "top_logp", at::kFloat, {m.rows, top}), w.p, w.bytes, queue(a[9]));
+                       (const int64_t*)vector(dev, a[1], "targets", at::kLong, {m.rows}), (int)top,
+                       (float*)vector(dev, a[2], "logp", at::kFloat, {m.rows}),
+                       (float*)vector(dev, a[3], "entropy", at::kFloat, {m.rows}),
+                       (float*)vector(dev, a[4], "stat", at::kFloat, {m.rows, 2}),
+                       (int32_t*)vector(dev, a[5], "top_ids", at::kInt, {m.rows, top}),
+                       (float*)vector(dev, a[6], "top_logp", at::kFloat, {m.rows, top}), w.p, w.bytes, queue(a[9]));
   });
 }
 
-Matrix gradient(PyObject* o, int code, const Matrix& like) {
+Matrix gradient(Device& dev, PyObject* o, int code, const Matrix& like) {
   const at::Tensor& t = tensor(o, "dlogits");
-  if (elem(t, "dlogits") != code) refuse(PyExc_ValueError, "dlogits must have the type of the logits");
+  if (elem(dev, t, "dlogits") != code) refuse(PyExc_ValueError, "dlogits must have the type of the logits");
   return matrix(t, "dlogits", like.rows, like.cols);
 }
 
 // logits, targets, g_logp, g_entropy, dlogits, logp, entropy, stat, scale, work, stream
 PyObject* logprobs_train(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 11, [&] {
+    Device dev;
     const at::Tensor& x = tensor(a[0], "logits");
-    const int code = elem(x, "logits");
-    const Matrix m = matrix(x, "logits"), d = gradient(a[4], code, m);
+    const int code = elem(dev, x, "logits");
+    const Matrix m = matrix(x, "logits"), d = gradient(dev, a[4], code, m);
     Work w;
-    w.take(a[9], nf_logprobs_work(code, m.rows, m.cols < 1 ? 1 : m.cols, 0, 1), x);
+    w.take(dev, a[9], nf_logprobs_work(code, m.rows, m.cols < 1 ? 1 : m.cols, 0, 1), x);
     return call(nf_logprobs_train, m.p, code, m.rows, m.cols, m.ld, (float)number(a[8]),
-                             (const int64_t*)vector(a[1], "targets", at::kLong, {m.rows}),
-                             (const float*)vector(a[2], "g_logp", at::kFloat, {m.rows}),
-                             (const float*)vector(a[3], "g_entropy", at::kFloat, {m.rows}),
-                             (float*)vector(a[5], "logp", at::kFloat, {m.rows}),
-                             (float*)vector(a[6], "entropy", at::kFloat, {m.rows}),
-                             (float*)vector(a[7], "stat", at::kFloat, {m.rows, 2}), d.p, d.ld, w.p, w.bytes, queue(a[10]));
+                             (const int64_t*)vector(dev, a[1], "targets", at::kLong, {m.rows}),
+                             (const float*)vector(dev, a[2], "g_logp", at::kFloat, {m.rows}),
+                             (const float*)vector(dev, a[3], "g_entropy", at::kFloat, {m.rows}),
+                             (float*)vector(dev, a[5], "logp", at::kFloat, {m.rows}),
+                             (float*)vector(dev, a[6], "entropy", at::kFloat, {m.rows}),
+                             (float*)vector(dev, a[7], "stat", at::kFloat, {m.rows, 2}), d.p, d.ld, w.p, w.bytes, queue(a[10]));
   });
 }
 
 // logits, targets, stat, entropy, g_logp, g_entropy, dlogits, scale, stream
 PyObject* logprobs_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 9, [&] {
+    Device dev;
     const at::Tensor& x = tensor(a[0], "logits");
-    const int code = elem(x, "logits");
-    const Matrix m = matrix(x, "logits"), d = gradient(a[6], code, m);
+    const int code = elem(dev, x, "logits");
+    const Matrix m = matrix(x, "logits"), d = gradient(dev, a[6], code, m);
     return call(nf_logprobs_grad, m.p, code, m.rows, m.cols, m.ld, (float)number(a[7]),
-                            (const int64_t*)vector(a[1], "targets", at::kLong, {m.rows}),
-                            (const float*)vector(a[2], "stat", at::kFloat, {m.rows, 2}),
-                            (const float*)vector(a[3], "entropy", at::kFloat, {m.rows}),
-                            (const float*)vector(a[4], "g_logp", at::kFloat, {m.rows}),
-                            (const float*)vector(a[5], "g_entropy", at::kFloat, {m.rows}), d.p, d.ld, queue(a[8]));
+                            (const int64_t*)vector(dev, a[1], "targets", at::kLong, {m.rows}),
+                            (const float*)vector(dev, a[2], "stat", at::kFloat, {m.rows, 2}),
+                            (const float*)vector(dev, a[3], "entropy", at::kFloat, {m.rows}),
+                            (const float*)vector(dev, a[4], "g_logp", at::kFloat, {m.rows}),
+                            (const float*)vector(dev, a[5], "g_entropy", at::kFloat, {m.rows}), d.p, d.ld, queue(a[8]));
   });
 }
 
@@ -243,14 +258,15 @@ Stack stack(const at::Tensor& t, const char* name) {
 // x, out, work, stream
 PyObject* orthogonalize(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 4, [&] {
+    Device dev;
     const at::Tensor &x = tensor(a[0], "x"), &out = tensor(a[1], "out");
-    const int code = elem(x, "x");
-    if (elem(out, "out") != code || out.sizes() != x.sizes()) refuse(PyExc_ValueError, "out must have x's type and shape");
+    const int code = elem(dev, x, "x");
+    if (elem(dev, out, "out") != code || out.sizes() != x.sizes()) refuse(PyExc_ValueError, "out must have x's type and shape");
     const Stack s = stack(x, "x"), o = stack(out, "out");
     Work w;
     const int64_t need = nf_orthogonalize_work(code, s.count, s.rows, s.cols);
     if (need < 0) return (int)NF_ESHAPE;
-    w.take(a[2], need, x);
+    w.take(dev, a[2], need, x);
     return call(nf_orthogonalize, s.p, code, s.count, s.rows, s.cols, s.ld, s.stride, o.p, o.ld, o.stride, w.p, w.bytes,
                                  queue(a[3]));
   });
@@ -259,19 +275,20 @@ PyObject* orthogonalize(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // w, m, g, w_out, m_out, eta, momentum, nesterov, decay, work, stream
 PyObject* muon_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 11, [&] {
+    Device dev;
     const at::Tensor &w = tensor(a[0], "w"), &g = tensor(a[2], "g");
-    const int wc = elem(w, "w"), gc = elem(g, "g");
+    const int wc = elem(dev, w, "w"), gc = elem(dev, g, "g");
     const auto shape = w.sizes();
     const Stack s = stack(w, "w");
-    void* const wp = whole(w, "w", w.scalar_type(), shape);
-    void* const gp = whole(g, "g", g.scalar_type(), shape);
-    void* const mp = whole(tensor(a[1], "m"), "m", at::kFloat, shape);
-    void* const wo = whole(tensor(a[3], "w_out"), "w_out", w.scalar_type(), shape);
-    void* const mo = whole(tensor(a[4], "m_out"), "m_out", at::kFloat, shape);
+    void* const wp = whole(dev, w, "w", w.scalar_type(), shape);
+    void* const gp = whole(dev, g, "g", g.scalar_type(), shape);
+    void* const mp = whole(dev, tensor(a[1], "m"), "m", at::kFloat, shape);
+    void* const wo = whole(dev, tensor(a[3], "w_out"), "w_out", w.scalar_type(), shape);
+    void* const mo = whole(dev, tensor(a[4], "m_out"), "m_out", at::kFloat, shape);
     Work k;
     const int64_t need = nf_orthogonalize_work(wc, s.count, s.rows, s.cols);
     if (need < 0) return (int)NF_ESHAPE;
-    k.take(a[9], need, w);
+    k.take(dev, a[9], need, w);
     return call(nf_muon_step, wp, wc, (const float*)mp, gp, gc, s.count, s.rows, s.cols, (float)number(a[5]),
                              (float)number(a[6]), (int)whole_number(a[7]), (float)number(a[8]), wo, (float*)mo, k.p,
                              k.bytes, queue(a[10]));
@@ -283,29 +300,31 @@ int64_t whole16(int64_t v) { return (v + 15) / 16 * 16; }
 // x, q, scale, stream
 PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 4, [&] {
+    Device dev;
     const at::Tensor& x = tensor(a[0], "x");
-    const int code = elem(x, "x");
-    const Matrix m = matrix(x, "x"), q = bytes_matrix(a[1], "q");
+    const int code = elem(dev, x, "x");
+    const Matrix m = matrix(x, "x"), q = bytes_matrix(dev, a[1], "q");
     if (q.rows != m.rows || q.cols < whole16(m.cols))
       refuse(PyExc_ValueError, "q must have x's rows and columns, these up to a multiple of 16");
     return call(nf_quantize_rows, m.p, code, m.rows, m.cols, m.ld, (int8_t*)q.p, q.ld,
-                            (float*)vector(a[2], "scale", at::kFloat, {m.rows}), queue(a[3]));
+                            (float*)vector(dev, a[2], "scale", at::kFloat, {m.rows}), queue(a[3]));
   });
 }
 
 // xq, x_scale, wq, w_scale, y, inputs, bias, act, stream
 PyObject* linear_i8(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 9, [&] {
-    const Matrix x = bytes_matrix(a[0], "xq"), w = bytes_matrix(a[2], "wq");
+    Device dev;
+    const Matrix x = bytes_matrix(dev, a[0], "xq"), w = bytes_matrix(dev, a[2], "wq");
     const int64_t inputs = whole_number(a[5]);
     if (x.cols < whole16(inputs) || w.cols < whole16(inputs))
       refuse(PyExc_ValueError, "xq and wq must hold the inputs, up to a multiple of 16");
     const at::Tensor& yt = tensor(a[4], "y");
-    const int yc = elem(yt, "y");
+    const int yc = elem(dev, yt, "y");
     const Matrix y = matrix(yt, "y", x.rows, w.rows);
-    return call(nf_linear_i8, (const int8_t*)x.p, x.ld, (const float*)vector(a[1], "x_scale", at::kFloat, {x.rows}),
-                        (const int8_t*)w.p, w.ld, (const float*)vector(a[3], "w_scale", at::kFloat, {w.rows}),
-                        (const float*)vector(a[6], "bias", at::kFloat, {w.rows}), (int)whole_number(a[7]), x.rows, inputs,
+    return call(nf_linear_i8, (const int8_t*)x.p, x.ld, (const float*)vector(dev, a[1], "x_scale", at::kFloat, {x.rows}),
+                        (const int8_t*)w.p, w.ld, (const float*)vector(dev, a[3], "w_scale", at::kFloat, {w.rows}),
+                        (const float*)vector(dev, a[6], "bias", at::kFloat, {w.rows}), (int)whole_number(a[7]), x.rows, inputs,
                         w.rows, y.p, yc, y.ld, queue(a[8]));
   });
 }
@@ -313,17 +332,18 @@ PyObject* linear_i8(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // x, wq, w_scale, y, bias, act, work, stream
 PyObject* linear_i8_dynamic(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 8, [&] {
+    Device dev;
     const at::Tensor &xt = tensor(a[0], "x"), &yt = tensor(a[3], "y");
-    const int xc = elem(xt, "x"), yc = elem(yt, "y");
-    const Matrix x = matrix(xt, "x"), w = bytes_matrix(a[1], "wq");
+    const int xc = elem(dev, xt, "x"), yc = elem(dev, yt, "y");
+    const Matrix x = matrix(xt, "x"), w = bytes_matrix(dev, a[1], "wq");
     if (w.cols < whole16(x.cols)) refuse(PyExc_ValueError, "wq must hold x's columns, up to a multiple of 16");
     const Matrix y = matrix(yt, "y", x.rows, w.rows);
-    const auto* ws = (const float*)vector(a[2], "w_scale", at::kFloat, {w.rows});
-    const auto* bs = (const float*)vector(a[4], "bias", at::kFloat, {w.rows});
+    const auto* ws = (const float*)vector(dev, a[2], "w_scale", at::kFloat, {w.rows});
+    const auto* bs = (const float*)vector(dev, a[4], "bias", at::kFloat, {w.rows});
     Work k;
     const int64_t need = nf_linear_i8_work(x.rows, x.cols);
     if (need < 0) return (int)NF_ESHAPE;
-    k.take(a[6], need, xt);
+    k.take(dev, a[6], need, xt);
     return call(nf_linear_i8_dynamic, x.p, xc, x.ld, (const int8_t*)w.p, w.ld, ws, bs, (int)whole_number(a[5]), x.rows,
                                      x.cols, w.rows, y.p, yc, y.ld, k.p, k.bytes, queue(a[7]));
   });
