@@ -13,6 +13,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdarg>
+#include <initializer_list>
 
 #include "nf.h"
 
@@ -152,6 +153,18 @@ struct Work {
   }
 };
 
+// A call's status, once the tensors that it wrote have a new version: what autograd kept of
+// their values before is no longer there.
+int wrote(std::initializer_list<PyObject*> outs, int st) {
+  if (st == NF_OK)
+    for (PyObject* o : outs)
+      if (o != Py_None) {
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+      }
+  return st;
+}
+
 double number(PyObject* o) {
   const double v = PyFloat_AsDouble(o);
   if (v == -1.0 && PyErr_Occurred()) throw Raised();
@@ -189,13 +202,14 @@ PyObject* logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (top > NF_TOP_MAX) top = NF_TOP_MAX + 1;            // refused below
     Work w;
     w.take(dev, a[8], nf_logprobs_work(code, m.rows, m.cols < 1 ? 1 : m.cols, (int)(top > NF_TOP_MAX ? 0 : top), 0), x);
-    return call(nf_logprobs, m.p, code, m.rows, m.cols, m.ld, (float)number(a[7]),
-                       (const int64_t*)vector(dev, a[1], "targets", at::kLong, {m.rows}), (int)top,
-                       (float*)vector(dev, a[2], "logp", at::kFloat, {m.rows}),
-                       (float*)vector(dev, a[3], "entropy", at::kFloat, {m.rows}),
-                       (float*)vector(dev, a[4], "stat", at::kFloat, {m.rows, 2}),
-                       (int32_t*)vector(dev, a[5], "top_ids", at::kInt, {m.rows, top}),
-                       (float*)vector(dev, a[6], "top_logp", at::kFloat, {m.rows, top}), w.p, w.bytes, queue(a[9]));
+    return wrote({a[2], a[3], a[4], a[5], a[6]},
+                 call(nf_logprobs, m.p, code, m.rows, m.cols, m.ld, (float)number(a[7]),
+                      (const int64_t*)vector(dev, a[1], "targets", at::kLong, {m.rows}), (int)top,
+                      (float*)vector(dev, a[2], "logp", at::kFloat, {m.rows}),
+                      (float*)vector(dev, a[3], "entropy", at::kFloat, {m.rows}),
+                      (float*)vector(dev, a[4], "stat", at::kFloat, {m.rows, 2}),
+                      (int32_t*)vector(dev, a[5], "top_ids", at::kInt, {m.rows, top}),
+                      (float*)vector(dev, a[6], "top_logp", at::kFloat, {m.rows, top}), w.p, w.bytes, queue(a[9])));
   });
 }
 
@@ -214,13 +228,14 @@ PyObject* logprobs_train(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Matrix m = matrix(x, "logits"), d = gradient(dev, a[4], code, m);
     Work w;
     w.take(dev, a[9], nf_logprobs_work(code, m.rows, m.cols < 1 ? 1 : m.cols, 0, 1), x);
-    return call(nf_logprobs_train, m.p, code, m.rows, m.cols, m.ld, (float)number(a[8]),
-                             (const int64_t*)vector(dev, a[1], "targets", at::kLong, {m.rows}),
-                             (const float*)vector(dev, a[2], "g_logp", at::kFloat, {m.rows}),
-                             (const float*)vector(dev, a[3], "g_entropy", at::kFloat, {m.rows}),
-                             (float*)vector(dev, a[5], "logp", at::kFloat, {m.rows}),
-                             (float*)vector(dev, a[6], "entropy", at::kFloat, {m.rows}),
-                             (float*)vector(dev, a[7], "stat", at::kFloat, {m.rows, 2}), d.p, d.ld, w.p, w.bytes, queue(a[10]));
+    return wrote({a[4], a[5], a[6], a[7]},
+                 call(nf_logprobs_train, m.p, code, m.rows, m.cols, m.ld, (float)number(a[8]),
+                      (const int64_t*)vector(dev, a[1], "targets", at::kLong, {m.rows}),
+                      (const float*)vector(dev, a[2], "g_logp", at::kFloat, {m.rows}),
+                      (const float*)vector(dev, a[3], "g_entropy", at::kFloat, {m.rows}),
+                      (float*)vector(dev, a[5], "logp", at::kFloat, {m.rows}),
+                      (float*)vector(dev, a[6], "entropy", at::kFloat, {m.rows}),
+                      (float*)vector(dev, a[7], "stat", at::kFloat, {m.rows, 2}), d.p, d.ld, w.p, w.bytes, queue(a[10])));
   });
 }
 
@@ -231,12 +246,13 @@ PyObject* logprobs_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor& x = tensor(a[0], "logits");
     const int code = elem(dev, x, "logits");
     const Matrix m = matrix(x, "logits"), d = gradient(dev, a[6], code, m);
-    return call(nf_logprobs_grad, m.p, code, m.rows, m.cols, m.ld, (float)number(a[7]),
-                            (const int64_t*)vector(dev, a[1], "targets", at::kLong, {m.rows}),
-                            (const float*)vector(dev, a[2], "stat", at::kFloat, {m.rows, 2}),
-                            (const float*)vector(dev, a[3], "entropy", at::kFloat, {m.rows}),
-                            (const float*)vector(dev, a[4], "g_logp", at::kFloat, {m.rows}),
-                            (const float*)vector(dev, a[5], "g_entropy", at::kFloat, {m.rows}), d.p, d.ld, queue(a[8]));
+    return wrote({a[6]},
+                 call(nf_logprobs_grad, m.p, code, m.rows, m.cols, m.ld, (float)number(a[7]),
+                      (const int64_t*)vector(dev, a[1], "targets", at::kLong, {m.rows}),
+                      (const float*)vector(dev, a[2], "stat", at::kFloat, {m.rows, 2}),
+                      (const float*)vector(dev, a[3], "entropy", at::kFloat, {m.rows}),
+                      (const float*)vector(dev, a[4], "g_logp", at::kFloat, {m.rows}),
+                      (const float*)vector(dev, a[5], "g_entropy", at::kFloat, {m.rows}), d.p, d.ld, queue(a[8])));
   });
 }
 
@@ -267,8 +283,9 @@ PyObject* orthogonalize(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t need = nf_orthogonalize_work(code, s.count, s.rows, s.cols);
     if (need < 0) return (int)NF_ESHAPE;
     w.take(dev, a[2], need, x);
-    return call(nf_orthogonalize, s.p, code, s.count, s.rows, s.cols, s.ld, s.stride, o.p, o.ld, o.stride, w.p, w.bytes,
-                                 queue(a[3]));
+    return wrote({a[1]},
+                 call(nf_orthogonalize, s.p, code, s.count, s.rows, s.cols, s.ld, s.stride, o.p, o.ld, o.stride, w.p, w.bytes,
+                      queue(a[3])));
   });
 }
 
@@ -289,9 +306,10 @@ PyObject* muon_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t need = nf_orthogonalize_work(wc, s.count, s.rows, s.cols);
     if (need < 0) return (int)NF_ESHAPE;
     k.take(dev, a[9], need, w);
-    return call(nf_muon_step, wp, wc, (const float*)mp, gp, gc, s.count, s.rows, s.cols, (float)number(a[5]),
-                             (float)number(a[6]), (int)whole_number(a[7]), (float)number(a[8]), wo, (float*)mo, k.p,
-                             k.bytes, queue(a[10]));
+    return wrote({a[3], a[4]},
+                 call(nf_muon_step, wp, wc, (const float*)mp, gp, gc, s.count, s.rows, s.cols, (float)number(a[5]),
+                      (float)number(a[6]), (int)whole_number(a[7]), (float)number(a[8]), wo, (float*)mo, k.p,
+                      k.bytes, queue(a[10])));
   });
 }
 
@@ -306,8 +324,9 @@ PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Matrix m = matrix(x, "x"), q = bytes_matrix(dev, a[1], "q");
     if (q.rows != m.rows || q.cols < whole16(m.cols))
       refuse(PyExc_ValueError, "q must have x's rows and columns, these up to a multiple of 16");
-    return call(nf_quantize_rows, m.p, code, m.rows, m.cols, m.ld, (int8_t*)q.p, q.ld,
-                            (float*)vector(dev, a[2], "scale", at::kFloat, {m.rows}), queue(a[3]));
+    return wrote({a[1], a[2]},
+                 call(nf_quantize_rows, m.p, code, m.rows, m.cols, m.ld, (int8_t*)q.p, q.ld,
+                      (float*)vector(dev, a[2], "scale", at::kFloat, {m.rows}), queue(a[3])));
   });
 }
 
@@ -322,10 +341,11 @@ PyObject* linear_i8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor& yt = tensor(a[4], "y");
     const int yc = elem(dev, yt, "y");
     const Matrix y = matrix(yt, "y", x.rows, w.rows);
-    return call(nf_linear_i8, (const int8_t*)x.p, x.ld, (const float*)vector(dev, a[1], "x_scale", at::kFloat, {x.rows}),
-                        (const int8_t*)w.p, w.ld, (const float*)vector(dev, a[3], "w_scale", at::kFloat, {w.rows}),
-                        (const float*)vector(dev, a[6], "bias", at::kFloat, {w.rows}), (int)whole_number(a[7]), x.rows, inputs,
-                        w.rows, y.p, yc, y.ld, queue(a[8]));
+    return wrote({a[4]},
+                 call(nf_linear_i8, (const int8_t*)x.p, x.ld, (const float*)vector(dev, a[1], "x_scale", at::kFloat, {x.rows}),
+                      (const int8_t*)w.p, w.ld, (const float*)vector(dev, a[3], "w_scale", at::kFloat, {w.rows}),
+                      (const float*)vector(dev, a[6], "bias", at::kFloat, {w.rows}), (int)whole_number(a[7]), x.rows, inputs,
+                      w.rows, y.p, yc, y.ld, queue(a[8])));
   });
 }
 
@@ -344,8 +364,9 @@ PyObject* linear_i8_dynamic(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t need = nf_linear_i8_work(x.rows, x.cols);
     if (need < 0) return (int)NF_ESHAPE;
     k.take(dev, a[6], need, xt);
-    return call(nf_linear_i8_dynamic, x.p, xc, x.ld, (const int8_t*)w.p, w.ld, ws, bs, (int)whole_number(a[5]), x.rows,
-                                     x.cols, w.rows, y.p, yc, y.ld, k.p, k.bytes, queue(a[7]));
+    return wrote({a[3]},
+                 call(nf_linear_i8_dynamic, x.p, xc, x.ld, (const int8_t*)w.p, w.ld, ws, bs, (int)whole_number(a[5]), x.rows,
+                      x.cols, w.rows, y.p, yc, y.ld, k.p, k.bytes, queue(a[7])));
   });
 }
 

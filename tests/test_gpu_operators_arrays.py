@@ -170,3 +170,24 @@ def _rand_rows(rows, classes):
         n = min(rows - r, 4099 * 1024)
         x[r:r + n].copy_(some.repeat((n + 4098) // 4099, 1)[:n])
     return x
+
+
+def test_overwritten_values_are_not_differentiated():
+    """Backpropagation through values that an operator has overwritten is refused."""
+    torch, nf = torch_cuda(), _nf()
+    note("versions")
+    x = _rand(6, 9).requires_grad_()
+    z = x.exp()                                           # keeps its result
+    t, g = torch.zeros(6, dtype=torch.int64, device="cuda"), _rand(6)
+    nf.nf_logprobs_train(z.detach(), t, g, None, z.detach())
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        z.sum().backward()
+    q, scale, y = torch.zeros((6, 16), dtype=torch.int8, device="cuda"), torch.empty(6, device="cuda"), torch.empty(3, 6, device="cuda")
+    nf.nf_quantize_rows(x.detach(), q, scale)
+    nf.nf_linear_i8_dynamic(_rand(3, 9), q, scale, y)
+    nf.nf_linear_i8(q, scale, q, scale, torch.empty(6, 6, device="cuda"), 9)
+    assert (q._version, scale._version, y._version) == (1, 1, 1)
+    with torch.inference_mode():
+        y = torch.empty(3, 6, device="cuda")
+        nf.nf_linear_i8_dynamic(_rand(3, 9), q, scale, y)
+    torch.cuda.synchronize()

@@ -94,3 +94,21 @@ def test_tensors_of_the_current_gpu_pass(bind, call):
 def test_tensors_of_another_gpu_are_refused(bind, call, name):
     with pytest.raises(ValueError, match=f"{name} is not on the current device"):
         getattr(bind, call)(*_args(call, name)[0])
+
+
+@pytest.mark.parametrize("call", [c for c in CALLS if not c.startswith("linear")])
+def test_written_tensors_have_a_new_version(bind, call):
+    args, written = _args(call)
+    if call == "logprobs":                                # without alternatives
+        args[5] = args[6] = None
+        written = written[:3]
+    before = [t._version for t in args if isinstance(t, torch.Tensor)]
+    assert getattr(bind, call)(*args) == nf.NF_OK
+    after = [t._version for t in args if isinstance(t, torch.Tensor)]
+    raised = [any(t is w for w in written) for t in args if isinstance(t, torch.Tensor)]
+    assert [b - a for a, b in zip(before, after)] == [int(r) for r in raised]
+
+
+def test_refused_calls_leave_versions(bind):
+    args, written = _args("linear_i8_dynamic")
+    assert bind.linear_i8_dynamic(*args) == nf.NF_EINVAL and written[0]._version == 0
