@@ -15,7 +15,6 @@ a second one.  The Python binding imports torch before loading the library.
 from __future__ import annotations
 
 import concurrent.futures
-import importlib.util
 import os
 import shutil
 import subprocess
@@ -54,10 +53,36 @@ def hipcc() -> str:
     raise RuntimeError("hipcc not found (ROCm is required to build the library)")
 
 
-def torch_dir():
-    """Where torch is installed (found without importing it); None where it is not."""
-    spec = importlib.util.find_spec("torch")
-    return os.path.dirname(spec.origin) if spec and spec.origin else None
+def cxx():
+    """A host C++ compiler; None where there is none."""
+    for cand in (os.environ.get("CXX"), "g++", "c++", "/opt/rocm/llvm/bin/clang++"):
+        if cand and shutil.which(cand):
+            return shutil.which(cand)
+    return None
+
+
+def bind_commands(obj: str, out: str):
+    """How the binding of the operators with tensors is compiled and linked; or, as a
+    text, what it lacks here.  The library and its nets need none of it."""
+    try:
+        import torch
+    except Exception as e:
+        return f"torch cannot be imported ({e})"
+    include = sysconfig.get_paths()["include"]
+    if cxx() is None:
+        return "there is no host C++ compiler"
+    if not os.path.exists(os.path.join(include, "Python.h")):
+        return f"Python's headers are not in {include}"
+    home = os.path.dirname(torch.__file__)
+    compile_ = [cxx(), "-O2", "-std=c++17", "-fPIC", "-Wall",
+                f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+                "-I", include, "-I", os.path.join(ROOT, "include"), "-isystem", os.path.join(home, "include"),
+                "-isystem", os.path.join(home, "include", "torch", "csrc", "api", "include"),
+                "-c", os.path.join(OPS, "nf_bind.cpp"), "-o", obj]
+    link = [cxx(), "-shared", "-fPIC", obj, "-o", out, "-L", os.path.dirname(LIB), "-l:" + os.path.basename(LIB),
+            "-L", os.path.join(home, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath,$ORIGIN",
+            "-Wl,-rpath," + os.path.join(home, "lib")]
+    return compile_, link
 
 
 def _run(cmd, verbose):
@@ -76,31 +101,28 @@ def build(verbose: bool = False) -> str:
     objs = [os.path.join(objdir, os.path.splitext(os.path.basename(p))[0] + ".o") for p in paths]
     cmds = [[hipcc(), *HIPCC_FLAGS, "-c", "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-I", OPS,
              path, "-o", obj] for path, obj in zip(paths, objs)]
-    torch = torch_dir()
-    bind = os.path.join(objdir, "nf_bind.o")
-    if torch:
-        cmds.append(["g++", "-O2", "-std=c++17", "-fPIC", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=1",
-                     "-I", sysconfig.get_paths()["include"], "-I", os.path.join(ROOT, "include"),
-                     "-isystem", os.path.join(torch, "include"),
-                     "-isystem", os.path.join(torch, "include", "torch", "csrc", "api", "include"),
-                     "-c", os.path.join(OPS, "nf_bind.cpp"), "-o", bind])
+    tmp_bind = BIND + ".tmp"
+    bind = bind_commands(os.path.join(objdir, "nf_bind.o"), tmp_bind)
     # one compiler process per source, at most as many as the CPUs this
     # process may use
     workers = max(1, min(len(cmds), len(os.sched_getaffinity(0)), 8))
     with concurrent.futures.ThreadPoolExecutor(workers) as pool:
+        bound = pool.submit(_run, bind[0], verbose) if not isinstance(bind, str) else None
         for f in [pool.submit(_run, c, verbose) for c in cmds]:
             f.result()
     rocm_lib = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(hipcc()))), "lib")
     tmp = LIB + ".tmp"
     _run([hipcc(), "-shared", "-fPIC", *objs, "-o", tmp, f"-Wl,-rpath,{rocm_lib}"], verbose)
     os.replace(tmp, LIB)
-    if torch is None:                       # no tensors to call the operators with
+    # one of an earlier build would not be this library's
+    if os.path.exists(BIND):
+        os.remove(BIND)
+    if bound is None:
+        print(f"no operators on tensors: {bind}", file=sys.stderr)
         return LIB
-    tmp = BIND + ".tmp"
-    _run(["g++", "-shared", "-fPIC", bind, "-o", tmp, "-L", HERE, "-l:" + os.path.basename(LIB),
-          "-L", os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath,$ORIGIN",
-          "-Wl,-rpath," + os.path.join(torch, "lib")], verbose)
-    os.replace(tmp, BIND)
+    bound.result()
+    _run(bind[1], verbose)
+    os.replace(tmp_bind, BIND)
     return LIB
 
 

@@ -424,15 +424,22 @@ NF_TOP_MAX, NF_ORTH_MAX, NF_ORTH_MAX_LD, NF_ORTH_STEPS = 64, 65536, 1 << 20, 5
 NF_LINEAR_I8_MAX, NF_NO_ACT = 131071, -1
 
 
+class _Missing:
+    """In _nfbind's place: the operators on tensors raise, the nets do without."""
+
+    def __init__(self, why: str):
+        self._why = why
+
+    def __getattr__(self, name):
+        raise ImportError(self._why)
+
+
 try:
     import torch
-except ImportError:
-    pass
-else:
-    if not os.path.exists(os.path.join(_HERE, "_nfbind.so")):
-        raise ImportError("_nfbind.so is missing: build the library first "
-                          "(python -m paper_1902_06714_amd.build, or __graft_entry__.build())")
     from . import _nfbind
+except ImportError as e:
+    _nfbind = _Missing(f"the operators on tensors need torch and _nfbind.so ({e}): build the library first "
+                       "(python -m paper_1902_06714_amd.build, or __graft_entry__.build())")
 
 
 def _on(stream, work, need, *args):
