@@ -127,10 +127,12 @@ struct Slope {
   bool entropies;
   // a row that `has` a target of log probability, and its sums
   __device__ __forceinline__ void set(float row_m, float ln, float entropy, float gi, float hi, float scale, bool none) {
-    // (of a row without probabilities every p is exp(-infinity))
+    // (of a row without probabilities every p is exp(-infinity), and no weight counts:
+    // one made from its log probability may be no number)
+    if (none) gi = hi = 0.f;
     m = none ? 0.f : row_m;
     k = none ? -__builtin_inff() : -ln * LOG2E;
-    own = none ? 0.f : scale * gi;
+    own = scale * gi;
     g = -scale * gi;
     h = -scale * hi;
     add = none ? 0.f : entropy - ln;

@@ -1,5 +1,5 @@
-"""The operators on arrays that lie in other arrays: results beside their inputs, in
-place, and what may not be."""
+"""The operators on arrays that lie in other arrays (results beside their inputs, in
+place, and what may not be), on very many rows, and on rows that nothing is left of."""
 
 import pytest
 
@@ -191,3 +191,35 @@ def test_overwritten_values_are_not_differentiated():
         y = torch.empty(3, 6, device="cuda")
         nf.nf_linear_i8_dynamic(_rand(3, 9), q, scale, y)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("rows,classes", [(5, 10), (5, 300), (300, 5000), (3, 40000), (2, 131072)])
+def test_rows_without_probabilities_have_no_gradient(rows, classes):
+    """... whatever their weights are: exp of the difference of two log probabilities of
+    minus infinity is NaN."""
+    torch, nf = torch_cuda(), _nf()
+    note(f"rows without probabilities, {rows}x{classes}")
+    inf, nan = float("inf"), float("nan")
+    x = _rand(rows, classes)
+    x[0] = -inf
+    x[-1] = -inf
+    t = torch.arange(rows, device="cuda")
+    logp, stat, entropy = torch.empty(rows, device="cuda"), torch.empty(rows, 2, device="cuda"), torch.empty(rows, device="cuda")
+    nf.nf_logprobs(x, t, logp=logp, stat=stat, entropy=entropy)
+    g = torch.exp(logp - logp.clone())                     # 1, and NaN where nothing is left
+    assert torch.isnan(g[0]) and torch.isnan(g[-1]) and (g[1:-1] == 1).all()
+    for h in (None, torch.ones(rows, device="cuda"), torch.full((rows,), nan, device="cuda"), torch.full((rows,), inf, device="cuda")):
+        both = []
+        for way in range(2):
+            dx = torch.full_like(x, 7.0)
+            if way:
+                nf.nf_logprobs_train(x, t, g, h, dx)
+            else:
+                nf.nf_logprobs_grad(x, t, stat, entropy, g, h, dx)
+            assert (dx[0] == 0).all() and (dx[-1] == 0).all()
+            both.append(dx)
+        if h is None:
+            assert all(torch.isfinite(dx).all() for dx in both)
+    t[0] = classes                                         # a target past the classes is told all the same
+    nf.nf_logprobs_train(x, t, g, None, dx)
+    assert torch.isnan(dx[0]).all() and (dx[-1] == 0).all()
