@@ -10,6 +10,7 @@ import pytest
 
 from oracle import operators as ref
 
+from .frames import Framed
 from .gpu_run import note, torch_cuda
 from .operator_sizes import LINEAR, MUON, ORTH
 
@@ -34,24 +35,6 @@ def _rand(shape, dtype, seed):
     gen = torch.Generator(device="cuda")
     gen.manual_seed(seed)
     return torch.randn(shape, generator=gen, device="cuda").to(_dt(dtype))
-
-
-class Framed:
-    """A GPU array of matrices whose rows lie `pad` apart, in an allocation that holds 7
-    wherever the array does not."""
-
-    def __init__(self, shape, dtype, pad, ahead=1):
-        torch = torch_cuda()
-        *count, rows, cols = shape
-        n = int(np.prod(count, dtype=np.int64)) if count else 1
-        self.flat = torch.full((ahead + n * rows * (cols + pad) + 64,), 7.0, device="cuda").to(_dt(dtype))
-        body = self.flat[ahead:ahead + n * rows * (cols + pad)]
-        self.view = body.view(*count, rows, cols + pad)[..., :cols]
-        self.inside = torch.zeros_like(self.flat, dtype=torch.bool)
-        self.inside[ahead:ahead + n * rows * (cols + pad)].view(*count, rows, cols + pad)[..., :cols] = True
-
-    def check(self):
-        assert (self.flat[~self.inside] == 7.0).all(), "written past the array"
 
 
 def _orthogonalised(u):
@@ -87,7 +70,7 @@ def test_orthogonalize(size, turned, dtype):
     count, rows, cols = (size[0], size[2], size[1]) if turned else size
     note(f"orthogonalize {count} x {rows} x {cols} {dtype}")
     x = _rand((count, rows, cols), dtype, rows)
-    out = Framed((count, rows, cols), dtype, 3)
+    out = Framed((count, rows, cols), _dt(dtype), 3)
     nf.nf_orthogonalize(x, out.view)
     torch.cuda.synchronize()
     out.check()
@@ -104,7 +87,7 @@ def test_muon_step(size, turned, w_dtype, g_dtype):
     note(f"muon {count} x {rows} x {cols} {w_dtype} {g_dtype}")
     shape = (count, rows, cols)
     w, g, m = _rand(shape, w_dtype, 1), _rand(shape, g_dtype, 2), _rand(shape, "f32", 3)
-    wo, mo = Framed(shape, w_dtype, 0), Framed(shape, "f32", 0)
+    wo, mo = Framed(shape, _dt(w_dtype), 0), Framed(shape, _dt("f32"), 0)
     eta, mu, decay = (float(np.float32(v)) for v in (0.05, 0.9, 0.2))
     nf.nf_muon_step(w, m, g, wo.view, mo.view, eta, mu, True, decay)
     torch.cuda.synchronize()
@@ -131,7 +114,7 @@ def test_linear(size, x_dtype, y_dtype):
     wq = torch.zeros((outputs, wide), dtype=torch.int8, device="cuda")
     wq[:, :inputs] = torch.randint(-128, 128, (outputs, inputs), device="cuda")
     ws, b = torch.rand(outputs, device="cuda") / (20 * inputs ** 0.5), _rand((outputs,), "f32", 6)
-    y = Framed((rows, outputs), y_dtype, 5)
+    y = Framed((rows, outputs), _dt(y_dtype), 5)
     nf.nf_linear_i8_dynamic(x, wq, ws, y.view, bias=b, act="relu")
     torch.cuda.synchronize()
     y.check()
