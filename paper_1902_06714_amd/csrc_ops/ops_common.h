@@ -39,11 +39,6 @@ __device__ __forceinline__ T from_float(float x) {
   }
 }
 
-template <class T>
-constexpr unsigned neg_inf_bits() {
-  return std::is_same_v<T, float> ? 0xff800000u : std::is_same_v<T, bf16_t> ? 0xff80u : 0xfc00u;
-}
-
 // 16 bytes of a row, at any address that its elements may have (the hardware
 // takes wide loads and stores at any alignment)
 template <class T>
