@@ -688,7 +688,9 @@ nf_status nf_orthogonalize(const void* d_x, int32_t dtype, int64_t count, int64_
   if (st == NF_OK) st = check_stack("the result", d_out, e, cols, ld_out);
   if (st == NF_OK) st = check_work(d_work, work_bytes, need);
   if (st != NF_OK) return st;
-  if (count > 1 && (stride < 0 || stride_out < (rows - 1) * ld_out + cols))
+  // results one behind another, or side by side in the same rows
+  if (count > 1 && (stride < 0 || (stride_out < (rows - 1) * ld_out + cols &&
+                                   (stride_out < cols || stride_out > (ld_out - cols) / (count - 1)))))
     return op_fail(NF_ESHAPE, "the results overlap one another");
   if (count == 1) stride = stride_out = 0;
   if (stride > INT64_MAX / 8 / count || stride_out > INT64_MAX / 8 / count)

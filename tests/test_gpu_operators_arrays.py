@@ -40,6 +40,24 @@ def test_orthogonalize_beside_its_matrices(rows, cols):
     assert torch.equal(turns[:, 0], want) and torch.equal(turns[:, 1], src)
 
 
+@pytest.mark.parametrize("rows,cols", [(90, 33), (30, 50), (70, 130)])
+def test_orthogonalize_matrices_side_by_side(rows, cols):
+    """A stack whose matrices are blocks of columns of one, as a layer's heads are."""
+    torch, nf = torch_cuda(), _nf()
+    note(f"orthogonalize side by side, {rows}x{cols}")
+    heads = _rand(rows, 4 * cols + 1)
+    x = heads[:, :4 * cols].view(rows, 4, cols).permute(1, 0, 2)
+    want = torch.empty(4, rows, cols, device="cuda")
+    nf.nf_orthogonalize(x, want)
+    out = torch.full((rows, 4, cols + 2), 7.0, device="cuda")
+    nf.nf_orthogonalize(x, out[:, :, :cols].permute(1, 0, 2))
+    last = heads[:, 4 * cols].clone()
+    nf.nf_orthogonalize(x, x)
+    torch.cuda.synchronize()
+    assert torch.equal(out[:, :, :cols].permute(1, 0, 2), want) and (out[:, :, cols:] == 7.0).all()
+    assert torch.equal(x, want) and torch.equal(heads[:, 4 * cols], last)
+
+
 @pytest.mark.parametrize("rows,cols", [(40, 70), (70, 130)])
 def test_orthogonalize_refuses_a_result_over_its_matrices(rows, cols):
     torch, nf = torch_cuda(), _nf()

@@ -10,7 +10,7 @@ import pytest
 
 from paper_1902_06714_amd import build, nf
 
-from .test_operators_cpu import E, GRAD, LOGP, MUON, ORTH, P, TRAIN, _call
+from .test_operators_cpu import E, GRAD, LOGP, MUON, ORTH, P, S, TRAIN, _call
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -28,6 +28,14 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 def test_orthogonalize_refuses_a_result_over_its_matrices(change):
     assert _call("nf_orthogonalize", ORTH, change) == E, nf.nf_last_error()
     assert "overlaps" in nf.nf_last_error()
+
+
+@pytest.mark.parametrize("change", [
+    {"so": 7, "ldo": 40}, {"so": 20, "ldo": 27}, {"so": 0, "ldo": 40}, {"so": -8, "ldo": 40}, {"so": 13, "ldo": 40, "count": 4},
+    {"so": 47, "count": 3}])
+def test_orthogonalize_refuses_results_over_one_another(change):
+    assert _call("nf_orthogonalize", ORTH, {"out": 99 * P, **change}) == S, nf.nf_last_error()
+    assert "overlap" in nf.nf_last_error()
 
 
 # new weights shifted on the gradient, or in its place with fp32 for bf16
