@@ -138,6 +138,7 @@ struct Work {
   at::Tensor keep;
   void* p = nullptr;
   int64_t bytes = 0;
+  // need: below 0 for sizes that the call refuses, which tells why
   void take(Device& dev, PyObject* o, int64_t need, const at::Tensor& like) {
     if (o == Py_None) {
       if (need <= 0) return;
@@ -280,9 +281,7 @@ PyObject* orthogonalize(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (elem(dev, out, "out") != code || out.sizes() != x.sizes()) refuse(PyExc_ValueError, "out must have x's type and shape");
     const Stack s = stack(x, "x"), o = stack(out, "out");
     Work w;
-    const int64_t need = nf_orthogonalize_work(code, s.count, s.rows, s.cols);
-    if (need < 0) return (int)NF_ESHAPE;
-    w.take(dev, a[2], need, x);
+    w.take(dev, a[2], nf_orthogonalize_work(code, s.count, s.rows, s.cols), x);
     return wrote({a[1]},
                  call(nf_orthogonalize, s.p, code, s.count, s.rows, s.cols, s.ld, s.stride, o.p, o.ld, o.stride, w.p, w.bytes,
                       queue(a[3])));
@@ -303,9 +302,7 @@ PyObject* muon_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void* const wo = whole(dev, tensor(a[3], "w_out"), "w_out", w.scalar_type(), shape);
     void* const mo = whole(dev, tensor(a[4], "m_out"), "m_out", at::kFloat, shape);
     Work k;
-    const int64_t need = nf_orthogonalize_work(wc, s.count, s.rows, s.cols);
-    if (need < 0) return (int)NF_ESHAPE;
-    k.take(dev, a[9], need, w);
+    k.take(dev, a[9], nf_orthogonalize_work(wc, s.count, s.rows, s.cols), w);
     return wrote({a[3], a[4]},
                  call(nf_muon_step, wp, wc, (const float*)mp, gp, gc, s.count, s.rows, s.cols, (float)number(a[5]),
                       (float)number(a[6]), (int)whole_number(a[7]), (float)number(a[8]), wo, (float*)mo, k.p,
@@ -361,9 +358,7 @@ PyObject* linear_i8_dynamic(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const auto* ws = (const float*)vector(dev, a[2], "w_scale", at::kFloat, {w.rows});
     const auto* bs = (const float*)vector(dev, a[4], "bias", at::kFloat, {w.rows});
     Work k;
-    const int64_t need = nf_linear_i8_work(x.rows, x.cols);
-    if (need < 0) return (int)NF_ESHAPE;
-    k.take(dev, a[6], need, xt);
+    k.take(dev, a[6], nf_linear_i8_work(x.rows, x.cols), xt);
     return wrote({a[3]},
                  call(nf_linear_i8_dynamic, x.p, xc, x.ld, (const int8_t*)w.p, w.ld, ws, bs, (int)whole_number(a[5]), x.rows,
                       x.cols, w.rows, y.p, yc, y.ld, k.p, k.bytes, queue(a[7])));

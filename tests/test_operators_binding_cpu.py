@@ -112,3 +112,21 @@ def test_written_tensors_have_a_new_version(bind, call):
 def test_refused_calls_leave_versions(bind):
     args, written = _args("linear_i8_dynamic")
     assert bind.linear_i8_dynamic(*args) == nf.NF_EINVAL and written[0]._version == 0
+
+
+@pytest.mark.parametrize("call,shape,dtype,status,says", [
+    ("orthogonalize", (0, 4, 7), torch.float16, nf.NF_EINVAL, "fp32 or bf16"),
+    ("orthogonalize", (0, 7), F32, nf.NF_EINVAL, "at least 1"), ("orthogonalize", (0, 4, 65537), F32, nf.NF_ESHAPE, "at most"),
+    ("muon_step", (0, 4, 7), torch.float16, nf.NF_EINVAL, "fp32 or bf16"),
+    ("muon_step", (2, 0, 7), F32, nf.NF_EINVAL, "at least 1"),
+    ("linear_i8_dynamic", (0, 0), F32, nf.NF_EINVAL, "at least"),
+    ("linear_i8_dynamic", (0, 131072), F32, nf.NF_ESHAPE, "at most")])
+def test_sizes_are_refused_with_the_librarys_own_status(bind, call, shape, dtype, status, says):
+    t = [gpu(shape, dtype) for _ in range(5)]
+    if call == "orthogonalize":
+        st = bind.orthogonalize(t[0], t[1], None, -1)
+    elif call == "muon_step":
+        st = bind.muon_step(t[0], gpu(shape), t[1], t[2], gpu(shape), 0.1, 0.9, 1, 0.0, None, -1)
+    else:
+        st = bind.linear_i8_dynamic(t[0], gpu((5, shape[1]), I8), gpu((5,)), gpu((0, 5)), None, -1, None, -1)
+    assert st == status and says in nf.nf_last_error(), (st, nf.nf_last_error())
