@@ -5,14 +5,18 @@
 //   log p_j = (z_j - m) - log s,   H = log s - sum exp(z - m) (z - m) / s,
 //   d(g log p_t + h H)/dx_j = scale (g ([j = t] - p_j) - h p_j (log p_j + H)).
 //
-// What bounds it: the bytes of the logits.  A row is read once into registers
-// where they hold it (up to 128 KB), so that the maximum, the sums, the
-// alternatives and the gradient all come from one read; a longer row is read
-// with a running maximum and sum, and again for each of the others.  Rows of at
-// most 128 classes take 8 to 64 lanes of a wave.  Measured (us): the loss with its gradient
-// of 4096 x 32768 bf16 114 (4.7 TB/s, a copy 5.0); scores of 2049 x 50021 bf16 with 8
-// alternatives 72 (2.8 TB/s: about 13 vector instructions a value beside an exponential bound
-// it); 10000 x 10 f32 4.3 and 1 x 32768 bf16 7.5 (a launch alone takes 3.5).
+// What bounds it: the bytes of the logits.  A row of up to 64 KB with a gradient or of at
+// most as many rows as compute units, and of up to 8 KB else, is read once into registers,
+// and the maximum, the sums, the alternatives and the gradient all come from that
+// read; a longer row is read with a running maximum and sum, and again for each of
+// the others.  Rows of at most 128 classes take 8 to 64 lanes of a wave.  Measured (us):
+// the loss with its gradient of 4096 x 32768 bf16 114 (4.7 TB/s, a copy 4.9 - 5.0); of rows
+// past 64 KB, whose second read does not all come from caches, 600 x 50000 bf16 40 where a read and a
+// write take 24, 1000 x 131072 bf16 171 for 105; 10000 x 10 f32 4.3 and 1 x 32768 bf16 7.5 (a launch
+// alone takes 3.5).  Scores of 2049 x 50021 bf16 with 8 alternatives 72 for 41 of bytes: 15 vector
+// instructions a value fill 56% of the issue cycles, and of the 6 waves a SIMD that 72 registers
+// leave room for 4.5 are there on average, too few for the loads and the instructions to hide
+// one another.
 //
 // Alternatives: ordered(z) is a whole number in z's order, so (ordered(z),
 // ~index) orders by value and then by the lower index, and no two are equal.

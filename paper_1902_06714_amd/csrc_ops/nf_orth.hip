@@ -25,10 +25,13 @@
 // rows.
 //
 // What bounds it, measured with all launches (us): the matrix cores at the card's power for
-// a step of 4096 x 4096 fp32, 3850 (1.07 PFLOP/s of f16 products, as a plain one of 4096
-// reaches); 17 launches of 7 - 14 for 1024 x 784 fp32, 167, and four of 517 x 1001 bf16, 157,
-// of which 3.5 each are the launch and most of the rest the way of a tile's operands into a few
-// compute units.
+// a step of 4096 x 4096 fp32, 3850 - 3890 (1.07 PFLOP/s of f16 products, as a plain one of 4096
+// reaches); for one of bf16, 1780 where its products at that rate take 1250, also the fp32 X's
+// bytes (0.93 PFLOP/s in the steps, 0.75 in X X^T, 77 of fill and sums); 17 launches of 7 - 14
+// for 1024 x 784 fp32, 167, and four of 517 x 1001 bf16, 157, of which 3.5 each are the launch
+// and most of the rest the way of a tile's operands into a few compute units.  The last
+// product of bf16 matrices in tiles of 128 does not fit its 128 registers and keeps 35 in scratch:
+// 48 for 3000 x 1500 where the steps before take 35.
 #include <cmath>
 
 #include "orth_small.h"

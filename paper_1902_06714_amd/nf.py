@@ -1,7 +1,8 @@
 """Binding of include/nf.h, by ctypes and for the operators on tensors by a small
-module of compiled code: the same entry points, argument marshalling only.  Every step of the computation runs in the HIP library; there is no
-other implementation behind these functions.  Importing this module fails
-loudly when the library has not been built.
+module of compiled code: the same entry points, argument marshalling only.  Every
+step of the computation runs in the HIP library; there is no other implementation
+behind these functions.  Importing this module fails loudly when the library has
+not been built, and calling an operator when the compiled module has not.
 
 Device buffers are passed as torch CUDA (HIP) tensors, which supply the device
 pointer; streams default to torch's current stream.  Tensors must be
@@ -418,8 +419,9 @@ def nf_calib_spin(us: float, stream=None) -> None:
 
 # -- operators on the caller's own tensors ------------------------------------
 # Matrices are 2-D (stacks 3-D) GPU tensors whose rows are contiguous; vectors
-# are contiguous.  Outputs are the caller's tensors; None leaves one out.  The
-# tensors are checked and taken apart in _nfbind (csrc_ops/nf_bind.cpp).
+# are contiguous, all on the current device.  Outputs are the caller's tensors; None
+# leaves one out; unless it is said otherwise they share no memory with one another or
+# with inputs.  The tensors are checked and taken apart in _nfbind (csrc_ops/nf_bind.cpp).
 NF_TOP_MAX, NF_ORTH_MAX, NF_ORTH_MAX_LD, NF_ORTH_STEPS = 64, 65536, 1 << 20, 5
 NF_LINEAR_I8_MAX, NF_NO_ACT = 131071, -1
 
@@ -521,7 +523,7 @@ def _stack_work(t):
 
 def nf_orthogonalize(x, out, work=None, stream=None) -> None:
     """x: a matrix [rows][cols] or a stack [count][rows][cols] in fp32 or bf16; out of the
-    same type and shape, or x itself."""
+    same type and shape, apart from x or x itself."""
     s, work = (-1, work) if stream is None else _on(stream, work, _stack_work, x)
     st = _nfbind.orthogonalize(x, out, work, s)
     if st:
@@ -531,7 +533,7 @@ def nf_orthogonalize(x, out, work=None, stream=None) -> None:
 def nf_muon_step(w, m, g, w_out, m_out, eta: float, momentum: float = 0.95, nesterov: bool = True,
                  decay: float = 0.0, work=None, stream=None) -> None:
     """One step on w ([rows][cols] or a stack) with gradient g and fp32 momentum m, into
-    w_out and m_out (which may be w and m).  All contiguous."""
+    w_out (which may be w, or g of the same type) and m_out (which may be m).  All contiguous."""
     s, work = (-1, work) if stream is None else _on(stream, work, _stack_work, w)
     st = _nfbind.muon_step(w, m, g, w_out, m_out, eta, momentum, nesterov, decay, work, s)
     if st:
