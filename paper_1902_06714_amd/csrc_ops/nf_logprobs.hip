@@ -33,7 +33,7 @@
 namespace nf {
 namespace {
 
-constexpr int TOP_MAX = 64;      // a wave's lanes hold enough maxima for the threshold
+static_assert(NF_TOP_MAX <= 64, "a wave's lanes hold enough maxima for the threshold");
 constexpr int TOP_CAP = 1024;    // candidates held in LDS
 constexpr int SMALL_MAX = 128;   // classes of the kernel that shares a wave among rows
 
